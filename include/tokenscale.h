@@ -159,6 +159,125 @@ int ts_mixed_paged_attention_noalloc(ts_ctx *ctx, void *stream,
                                      float sm_scale,
                                      void *out);
 
+/* ---- Rotary positions, drafted trees, moving and reading back cache entries ---------------------------------------
+ *
+ * A layer with rotary positions appends with ts_rope_kv_append and then runs ts_mixed_paged_attention with k_new = v_new =
+ * NULL.  A decoder that verifies drafted tokens appends the tree's nodes with it, runs ts_tree_attention, and brings the
+ * accepted path's entries together with ts_kv_move.  ts_kv_read hands cached K/V on as rows.
+ *
+ * Conventions as above, and: these calls allocate nothing on the device but ts_tree_attention's scratch (see
+ * ts_reserve_tree), use no pinned memory and keep no lists on the device, so all of them may be captured into a graph; a
+ * captured call fixes the HOST arrays' values.  A context orders its eager calls among streams; the replays of a graph are
+ * ordered by the caller.  "kernel_timing" counts the append, move and read under TS_K_APPEND, the tree attention under
+ * TS_K_DECODE and its merge under TS_K_COMBINE (eager calls only); "validate_block_table" is honoured, but refused under
+ * capture (TS_ERR_UNSUPPORTED).  None of them touches the velocity counters. */
+
+/* Rotation of a head's first rot_dim dims.  Pair i (0 <= i < rot_dim / 2) is turned by the angle position * f_i:
+ *   (x, y) -> m * (x cos - y sin, y cos + x sin)
+ * layout TS_ROPE_HALF pairs dims (i, i + rot_dim / 2), TS_ROPE_INTERLEAVED dims (2i, 2i + 1); dims from rot_dim on stay as
+ * they are.  With b_i = base ^ (-2i / rot_dim):
+ *   TS_ROPE_NONE        f_i = b_i
+ *   TS_ROPE_LINEAR      f_i = b_i / factor
+ *   TS_ROPE_NTK         f_i = (base * factor ^ (rot_dim / (rot_dim - 2))) ^ (-2i / rot_dim)   (rot_dim 2: f_0 = 1)
+ *   TS_ROPE_YARN        f_i = b_i (1 - r_i) + b_i / factor * r_i, r_i = clamp((i - lo) / max(hi - lo, 0.001), 0, 1), where
+ *                       d(t) = rot_dim ln(original_length / (2 pi t)) / (2 ln base) is the pair that makes t turns within
+ *                       the original length, lo = max(floor(d(high)), 0), hi = min(ceil(d(low)), rot_dim - 1); low and high
+ *                       0 select 1 and 32.  m = 1 + 0.1 ln(factor)
+ *   TS_ROPE_WAVELENGTH  f_i = b_i k_i + b_i / factor * (1 - k_i), k_i = clamp((t_i - low) / (high - low), 0, 1), t_i =
+ *                       original_length b_i / (2 pi) turns within the original length; low and high 0 select 1 and 4
+ *   TS_ROPE_TABLE       f_i = table[i]
+ * m = 1 where nothing else is said; attn_scale > 0 takes its place. */
+typedef enum { TS_ROPE_HALF = 0, TS_ROPE_INTERLEAVED = 1 } ts_rope_layout;
+typedef enum { TS_ROPE_NONE = 0, TS_ROPE_LINEAR = 1, TS_ROPE_NTK = 2, TS_ROPE_YARN = 3, TS_ROPE_WAVELENGTH = 4, TS_ROPE_TABLE = 5 } ts_rope_scaling;
+typedef struct {
+    int32_t rot_dim;               /* even, 2 .. head_dim */
+    int32_t layout, scaling;
+    int32_t original_length;       /* TS_ROPE_YARN, TS_ROPE_WAVELENGTH: > 0 */
+    double base;                   /* > 1 (not read with TS_ROPE_TABLE) */
+    double factor;                 /* scalings but NONE and TABLE: >= 1 */
+    double low, high;              /* 0 or 0 < low < high */
+    double attn_scale;             /* 0 = the scaling's own */
+    const double *table;           /* HOST [rot_dim / 2], TS_ROPE_TABLE only, finite */
+} ts_rope_desc;
+
+/* Host only.  Writes the rot_dim / 2 angles per position into freq and m into scale (either may be NULL).
+ * TS_ERR_INVALID_ARG for a description outside the stated domain. */
+int ts_rope_frequencies(const ts_rope_desc *rope, double *freq, double *scale);
+
+/* Sets the rotation of the context's layer for later ts_rope_kv_append calls (calls already made, captured ones included,
+ * keep theirs); NULL removes it.  Host only; the description and its table are consumed. */
+int ts_set_rope(ts_ctx *ctx, const ts_rope_desc *rope);
+
+/* Step a1 with rotary positions: rotates the new tokens' q and K and stores K and V into the paged cache, in one launch per
+ * 256 sequences.
+ *   q, k_new, v_new : DEV, token row t at t * stride elements (slices of one projection's output, say), its heads and dims
+ *                     packed [H, D] of q_dtype; stride 0 = packed rows, else at least H * D
+ *   q_out : DEV [T, Hq, D], may be q itself if its rows are packed, else must not overlap the inputs; q and q_out may both
+ *           be NULL (K and V only)
+ *   positions : DEV int32 [T], or NULL for the tokens' places in their sequences (prefix_s + i); a drafted tree's node has
+ *           position prefix_s + depth.  The place in the cache is prefix_s + i either way.
+ * The angle is formed in double precision, the rotation in single precision; q is rounded once to q_dtype, and K once
+ * to the cache's type (e4m3: of rotated / scale).  V goes as in ts_kv_append.
+ * Errors: as ts_kv_append; TS_ERR_INVALID_ARG without ts_set_rope, for a stride that is too small, and for q_out == q with
+ * rows that are not packed. */
+int ts_rope_kv_append(ts_ctx *ctx, void *stream,
+                      const void *q, int64_t q_stride,
+                      const void *k_new, int64_t k_stride,
+                      const void *v_new, int64_t v_stride,
+                      void *q_out, void *k_cache, void *v_cache,
+                      const float *k_scale, const float *v_scale,
+                      const int32_t *block_table, const int32_t *positions,
+                      const int32_t *q_lens, const int32_t *ctx_lens, int num_seqs);
+
+/* Attention of drafted trees: sequence s brings q_lens[s] nodes, whose K/V are its last q_lens[s] cache entries (node j
+ * at position prefix_s + j), and every node sees the prefix and the nodes that its mask names.
+ *   tree_mask : DEV uint64 [T, mask_words]: bit j % 64 of word j / 64 of row (s, i) = node i sees node j; bits from
+ *               q_lens[s] on are ignored.  A node that sees no key at all gets zeros.  NULL = chains: node i sees nodes 0 .. i
+ *               (mask_words is not read)
+ *   other arguments as in ts_mixed_paged_attention; q [T, Hq, D] and out [T, Hq, D] must be 16-byte aligned
+ * What a row does not see has no influence on it, whatever its value (infinities and NaN included).  A row whose visible
+ * scores are all -inf is NaN.  Softmax statistics and sums are held in single precision, the weights enter the second
+ * product in q_dtype.  Results are run-to-run identical.
+ * Errors: TS_ERR_INVALID_ARG as above and for too few mask words; TS_ERR_UNSUPPORTED for more than TS_TREE_MAX_NODES nodes. */
+#define TS_TREE_MAX_NODES 256
+int ts_tree_attention(ts_ctx *ctx, void *stream,
+                      const void *q, const void *k_cache, const void *v_cache,
+                      const float *k_scale, const float *v_scale,
+                      const int32_t *block_table,
+                      const uint64_t *tree_mask, int mask_words,
+                      const int32_t *q_lens, const int32_t *ctx_lens, int num_seqs,
+                      float sm_scale, void *out);
+
+/* Allocates ts_tree_attention's scratch (its size goes by the geometry, not by the batch: at most 160 MiB) if it is not there yet.
+ * Without it the first call that needs it allocates it, which fails with TS_ERR_UNSUPPORTED under capture. */
+int ts_reserve_tree(ts_ctx *ctx);
+
+/* Host only.  Masks and depths of trees given by parents: parents HOST int32 [T], node i's parent within its own tree, below
+ * i, or -1 for a root.  mask HOST uint64 [T, mask_words] (may be NULL): every node sees its ancestors and itself; depth HOST
+ * int32 [T] (may be NULL): roots have 0.  TS_ERR_INVALID_ARG for a parent out of range, a negative length, too few words. */
+int ts_tree_masks(const int32_t *parents, const int32_t *q_lens, int num_seqs, int mask_words, uint64_t *mask, int32_t *depth);
+
+/* Moves cache entries within their sequences (all KV heads, K and V): position dst[i] takes what position src[i] held before the
+ * call.  move_lens[s] pairs of sequence s, packed by sequence.
+ *   src, dst : DEV int32 [sum of move_lens]
+ *   move_lens, ctx_lens : HOST int32 [S]; a pair with a position outside [0, ctx_lens[s]) is skipped (-1 as padding); of
+ *                         several pairs with one dst the last counts
+ * Entries that move into a page that another sequence shares move for that sequence too.
+ * Errors: TS_ERR_INVALID_ARG for null pointers, negative lengths, ctx_lens beyond the table; TS_ERR_UNSUPPORTED for more than
+ * TS_MAX_MOVES pairs of a sequence. */
+#define TS_MAX_MOVES 64
+int ts_kv_move(ts_ctx *ctx, void *stream, void *k_cache, void *v_cache, const int32_t *block_table,
+               const int32_t *src, const int32_t *dst, const int32_t *move_lens, const int32_t *ctx_lens, int num_seqs);
+
+/* Reads cached tokens back as rows: positions starts[s] .. starts[s] + lens[s] - 1 of every sequence, packed by sequence.
+ *   k_out, v_out : DEV [sum of lens, Hkv, D] q_dtype; one of them may be NULL.  e4m3 elements are multiplied by their head's
+ *                  scale in single precision and rounded once
+ *   starts, lens : HOST int32 [S], starts may be NULL (0)
+ * Errors: TS_ERR_INVALID_ARG for null pointers, negative numbers, positions beyond the table. */
+int ts_kv_read(ts_ctx *ctx, void *stream, const void *k_cache, const void *v_cache,
+               const float *k_scale, const float *v_scale, const int32_t *block_table,
+               const int32_t *starts, const int32_t *lens, int num_seqs, void *k_out, void *v_out);
+
 /* Step a6 -- Token Velocity of this context (Sec. 3.2): tokens released per second, separately
  * for prefill chunks (rows of sequences with q_len > 1) and decode rows (q_len == 1), over the
  * window that started at the first pass after the last reset. */

@@ -16,7 +16,9 @@ TS_VELOCITY_RESET, TS_VELOCITY_SYNC = 1, 2
 
 EXPORTS = ["ts_check_desc", "ts_cache_bytes", "ts_create", "ts_destroy", "ts_reserve", "ts_kv_append",
            "ts_mixed_paged_attention", "ts_mixed_paged_attention_noalloc", "ts_token_velocity", "ts_last_error", "ts_set_option",
-           "ts_get_option", "ts_plan_describe", "ts_plan_export", "ts_kernel_times"]
+           "ts_get_option", "ts_plan_describe", "ts_plan_export", "ts_kernel_times",
+           "ts_rope_frequencies", "ts_set_rope", "ts_rope_kv_append", "ts_tree_attention", "ts_reserve_tree", "ts_tree_masks",
+           "ts_kv_move", "ts_kv_read"]
 CALIB_EXPORTS = ["ts_calib_copy", "ts_calib_read", "ts_calib_mfma"]     # include/tokenscale_calib.h
 
 KERNEL_NAMES = ["append", "decode", "combine", "prefill", "rows", "mixed"]
@@ -39,6 +41,36 @@ class Desc(ctypes.Structure):
         qd = DTYPES[q_dtype] if isinstance(q_dtype, str) else int(q_dtype)
         kd = DTYPES[kv_dtype] if isinstance(kv_dtype, str) else int(kv_dtype)
         return cls(Hq, Hkv, D, page_size, qd, kd, num_pages, max_pages_per_seq)
+
+
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3, "wavelength": 4, "table": 5}
+TREE_MAX_NODES, MAX_MOVES = 256, 64
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("scaling", ctypes.c_int32),
+                ("original_length", ctypes.c_int32), ("base", ctypes.c_double), ("factor", ctypes.c_double),
+                ("low", ctypes.c_double), ("high", ctypes.c_double), ("attn_scale", ctypes.c_double),
+                ("table", ctypes.c_void_p)]
+
+    @classmethod
+    def make(cls, rot_dim, base=10000.0, layout="half", scaling="none", factor=1.0, original_length=0, low=0.0, high=0.0,
+             attn_scale=0.0, table=None):
+        """table: the rot_dim / 2 angles per position, which select the scaling "table"."""
+        for name, known in ((layout, ROPE_LAYOUTS), (scaling, ROPE_SCALINGS)):
+            if isinstance(name, str) and name not in known:
+                raise ValueError(f"{name!r} is none of {sorted(known)}")
+        values = None
+        if table is not None:
+            scaling = "table"
+            values = np.ascontiguousarray(table, dtype=np.float64)
+            if values.shape != (int(rot_dim) // 2,):
+                raise ValueError(f"table has shape {values.shape}, expected {(int(rot_dim) // 2,)}")
+        d = cls(int(rot_dim), ROPE_LAYOUTS.get(layout, layout), ROPE_SCALINGS.get(scaling, scaling), int(original_length), base,
+                factor, low, high, attn_scale, values.ctypes.data if values is not None else None)
+        d._values = values                                 # (the description points into it)
+        return d
 
 
 class Velocity(ctypes.Structure):
@@ -111,6 +143,23 @@ def load_library():
     lib.ts_plan_export.restype = ctypes.c_int64
     lib.ts_kernel_times.argtypes = [vp, ctypes.POINTER(KernelStats), ctypes.c_int]
     lib.ts_kernel_times.restype = ctypes.c_int
+    lib.ts_rope_frequencies.argtypes = [ctypes.POINTER(RopeDesc), vp, vp]
+    lib.ts_rope_frequencies.restype = ctypes.c_int
+    lib.ts_set_rope.argtypes = [vp, ctypes.POINTER(RopeDesc)]
+    lib.ts_set_rope.restype = ctypes.c_int
+    lib.ts_rope_kv_append.argtypes = [vp, vp, vp, ctypes.c_int64, vp, ctypes.c_int64, vp, ctypes.c_int64, vp, vp, vp, vp, vp, vp, vp,
+                                      i32p, i32p, ctypes.c_int]
+    lib.ts_rope_kv_append.restype = ctypes.c_int
+    lib.ts_tree_attention.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_int, i32p, i32p, ctypes.c_int, ctypes.c_float, vp]
+    lib.ts_tree_attention.restype = ctypes.c_int
+    lib.ts_reserve_tree.argtypes = [vp]
+    lib.ts_reserve_tree.restype = ctypes.c_int
+    lib.ts_tree_masks.argtypes = [i32p, i32p, ctypes.c_int, ctypes.c_int, vp, i32p]
+    lib.ts_tree_masks.restype = ctypes.c_int
+    lib.ts_kv_move.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32p, i32p, ctypes.c_int]
+    lib.ts_kv_move.restype = ctypes.c_int
+    lib.ts_kv_read.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32p, i32p, ctypes.c_int, vp, vp]
+    lib.ts_kv_read.restype = ctypes.c_int
     lib.ts_calib_copy.argtypes = [vp, vp, vp, ctypes.c_int64]
     lib.ts_calib_copy.restype = ctypes.c_int
     lib.ts_calib_read.argtypes = [vp, vp, vp, ctypes.c_int64]
@@ -140,6 +189,21 @@ def _dev_ptr(t) -> int:
     if not t.is_contiguous():
         raise ValueError("tensor must be contiguous")
     return t.data_ptr()
+
+
+def _rows_ptr(t, heads: int, dim: int):
+    """(device pointer, elements from row to row) of token rows [T, heads, dim], whose heads and dims are packed."""
+    if t is None:
+        return 0, 0
+    if not t.is_cuda:
+        raise ValueError("expected a GPU tensor")
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
+        raise ValueError(f"rows of shape {tuple(t.shape)}, expected [tokens, {heads}, {dim}]")
+    if t.shape[0] == 0:
+        return 0, 0
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
+        raise ValueError("a row's heads and dims must be packed")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else 0
 
 
 def _i32_bytes(a) -> bytes:
@@ -199,6 +263,30 @@ def plan_decode_items(desc: Desc, q_lens, ctx_lens, split_pages: int = 0) -> np.
     return plan_export(desc, q_lens, ctx_lens, "decode", split_pages)[:, :5]
 
 
+def rope_frequencies(rot_dim: int, **kw):
+    """(angles per position of the rot_dim / 2 pairs, factor of cosine and sine); arguments as for Context.set_rope."""
+    desc = RopeDesc.make(rot_dim, **kw)
+    freq, scale = np.zeros(max(1, int(rot_dim) // 2)), ctypes.c_double(0.0)
+    rc = load_library().ts_rope_frequencies(ctypes.byref(desc), _np_ptr(freq), ctypes.byref(scale))
+    if rc != TS_OK:
+        raise TokenScaleError(rc, "ts_rope_frequencies")
+    return freq, float(scale.value)
+
+
+def tree_masks(parents, q_lens, mask_words: int = 0):
+    """(masks uint64 [T, mask_words], depths int32 [T]) of trees given by their nodes' parents (-1 = a root).  mask_words 0 = as
+    many as the largest tree needs.  torch has no use for uint64 here: hand masks over as masks.view(np.int64)."""
+    pa, ql = _i32(parents), _i32(q_lens)
+    if pa.size != int(ql.sum()):
+        raise ValueError(f"{pa.size} parents for {int(ql.sum())} nodes")
+    words = mask_words or max(1, -(-int(ql.max(initial=0)) // 64))
+    masks, depths = np.zeros((pa.size, words), np.uint64), np.zeros(pa.size, np.int32)
+    rc = load_library().ts_tree_masks(_np_ptr(pa), _np_ptr(ql), len(ql), words, _np_ptr(masks), _np_ptr(depths))
+    if rc != TS_OK:
+        raise TokenScaleError(rc, "ts_tree_masks")
+    return masks, depths
+
+
 _raw_stream = None
 
 
@@ -220,6 +308,9 @@ class Context:
     def __init__(self, desc: Desc, device: int = 0):
         self._lib = load_library()
         self.desc = desc
+        self.device = device
+        self._cache_bytes = cache_bytes(desc)
+        self._q_type = ("float32",) if desc.q_dtype == DTYPES["f32"] else ("bfloat16",)
         self._h = ctypes.c_void_p(0)
         rc = self._lib.ts_create(ctypes.byref(desc), device, ctypes.byref(self._h))
         if rc != TS_OK:
@@ -280,6 +371,104 @@ class Context:
         rc = fn(self._h, self._stream(stream), _dev_ptr(q), _dev_ptr(k_new), _dev_ptr(v_new),
                 _dev_ptr(k_cache), _dev_ptr(v_cache), _dev_ptr(k_scale), _dev_ptr(v_scale),
                 _dev_ptr(block_table), _i32_bytes(q_lens), _i32_bytes(ctx_lens), _count(q_lens), sm_scale, _dev_ptr(out))
+        if rc != TS_OK:
+            self._check(rc)
+
+    def set_rope(self, rot_dim: int, **kw):
+        """Rotation of this layer's heads for rope_kv_append: base, layout ("half" / "interleaved"), scaling ("none", "linear",
+        "ntk", "yarn", "wavelength") with factor, original_length, low, high, attn_scale; or table = angles per position."""
+        desc = RopeDesc.make(rot_dim, **kw)
+        self._check(self._lib.ts_set_rope(self._h, ctypes.byref(desc)))
+
+    @staticmethod
+    def _lens(first, *others):
+        """HOST int32 arrays of one length."""
+        got = [_i32(a).reshape(-1) for a in (first, *others)]
+        if any(a.size != got[0].size for a in got):
+            raise ValueError(f"lengths of {[a.size for a in got]} sequences")
+        return got
+
+    def _tensors(self, **named):
+        """Element types, sizes and device of tensors that are not only handed through: name = (tensor, element type, elements
+        or None)."""
+        for name, (t, dtype, n) in named.items():
+            if t is None or isinstance(t, int):
+                continue
+            if not t.is_cuda or t.device.index != self.device:
+                raise ValueError(f"{name} is on {t.device}, the context on GPU {self.device}")
+            if dtype and str(t.dtype).replace("torch.", "") not in dtype:
+                raise ValueError(f"{name} is {t.dtype}, expected {' or '.join(dtype)}")
+            if n is not None and t.numel() < n:
+                raise ValueError(f"{name} has {t.numel()} elements, needs {n}")
+
+    def _common(self, k_cache, v_cache, k_scale, v_scale, block_table, num_seqs):
+        need = self._cache_bytes
+        for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
+            if t is not None and not isinstance(t, int) and t.numel() * t.element_size() < need:
+                raise ValueError(f"{name} has {t.numel() * t.element_size()} bytes, needs {need}")
+        heads = self.desc.num_kv_heads
+        self._tensors(k_cache=(k_cache, None, None), v_cache=(v_cache, None, None), k_scale=(k_scale, ("float32",), heads),
+                      v_scale=(v_scale, ("float32",), heads),
+                      block_table=(block_table, ("int32",), num_seqs * self.desc.max_pages_per_seq))
+
+    def rope_kv_append(self, q, k_new, v_new, q_out, k_cache, v_cache, k_scale, v_scale, block_table, q_lens, ctx_lens,
+                       positions=None, stream=None):
+        """q, k_new, v_new: [T, heads, dim], rows may be strided (slices of one projection's output); q_out packed, may be q."""
+        d, (ql, cl) = self.desc, self._lens(q_lens, ctx_lens)
+        total, el = int(ql.sum()), self._q_type
+        self._common(k_cache, v_cache, k_scale, v_scale, block_table, ql.size)
+        self._tensors(q=(q, el, total * d.num_q_heads * d.head_dim), k_new=(k_new, el, total * d.num_kv_heads * d.head_dim),
+                      v_new=(v_new, el, total * d.num_kv_heads * d.head_dim), q_out=(q_out, el, total * d.num_q_heads * d.head_dim),
+                      positions=(positions, ("int32",), total))
+        q_rows, k_rows, v_rows = (_rows_ptr(t, h, d.head_dim) for t, h in ((q, d.num_q_heads), (k_new, d.num_kv_heads), (v_new, d.num_kv_heads)))
+        rc = self._lib.ts_rope_kv_append(self._h, self._stream(stream), *q_rows, *k_rows, *v_rows, _dev_ptr(q_out), _dev_ptr(k_cache),
+                                         _dev_ptr(v_cache), _dev_ptr(k_scale), _dev_ptr(v_scale), _dev_ptr(block_table),
+                                         _dev_ptr(positions), ql.tobytes(), cl.tobytes(), ql.size)
+        if rc != TS_OK:
+            self._check(rc)
+
+    def reserve_tree(self):
+        """Allocates tree_attention's scratch now (before a capture, say)."""
+        self._check(self._lib.ts_reserve_tree(self._h))
+
+    def tree_attention(self, q, k_cache, v_cache, k_scale, v_scale, block_table, tree_mask, q_lens, ctx_lens, sm_scale: float, out,
+                       stream=None):
+        """tree_mask: int64 [T, words] on the GPU (see tree_masks), or None for chains."""
+        d, (ql, cl) = self.desc, self._lens(q_lens, ctx_lens)
+        total, words = int(ql.sum()), 0
+        if tree_mask is not None:
+            if tree_mask.dim() != 2:
+                raise ValueError(f"tree_mask has shape {tuple(tree_mask.shape)}, expected [tokens, words]")
+            words = tree_mask.shape[1]
+        self._common(k_cache, v_cache, k_scale, v_scale, block_table, ql.size)
+        n = total * d.num_q_heads * d.head_dim
+        self._tensors(q=(q, self._q_type, n), out=(out, self._q_type, n), tree_mask=(tree_mask, ("int64", "uint64"), total * words))
+        rc = self._lib.ts_tree_attention(self._h, self._stream(stream), _dev_ptr(q), _dev_ptr(k_cache), _dev_ptr(v_cache),
+                                         _dev_ptr(k_scale), _dev_ptr(v_scale), _dev_ptr(block_table), _dev_ptr(tree_mask), words,
+                                         ql.tobytes(), cl.tobytes(), ql.size, sm_scale, _dev_ptr(out))
+        if rc != TS_OK:
+            self._check(rc)
+
+    def kv_move(self, k_cache, v_cache, block_table, src, dst, move_lens, ctx_lens, stream=None):
+        """Entries at positions dst take what positions src held; pairs packed by sequence, -1 = no pair."""
+        ml, cl = self._lens(move_lens, ctx_lens)
+        self._common(k_cache, v_cache, None, None, block_table, ml.size)
+        total = int(ml.sum())
+        self._tensors(src=(src, ("int32",), total), dst=(dst, ("int32",), total))
+        rc = self._lib.ts_kv_move(self._h, self._stream(stream), _dev_ptr(k_cache), _dev_ptr(v_cache), _dev_ptr(block_table), _dev_ptr(src),
+                                  _dev_ptr(dst), ml.tobytes(), cl.tobytes(), ml.size)
+        if rc != TS_OK:
+            self._check(rc)
+
+    def kv_read(self, k_cache, v_cache, k_scale, v_scale, block_table, starts, lens, k_out, v_out, stream=None):
+        """Tokens starts .. starts + lens - 1 of every sequence as rows [sum of lens, KV heads, dim]; starts None = 0."""
+        d, (ln, *first) = self.desc, self._lens(*((lens,) if starts is None else (lens, starts)))
+        self._common(k_cache, v_cache, k_scale, v_scale, block_table, ln.size)
+        n = int(ln.sum()) * d.num_kv_heads * d.head_dim
+        self._tensors(k_out=(k_out, self._q_type, n), v_out=(v_out, self._q_type, n))
+        rc = self._lib.ts_kv_read(self._h, self._stream(stream), _dev_ptr(k_cache), _dev_ptr(v_cache), _dev_ptr(k_scale), _dev_ptr(v_scale),
+                                  _dev_ptr(block_table), first[0].tobytes() if first else None, ln.tobytes(), ln.size,
+                                  _dev_ptr(k_out), _dev_ptr(v_out))
         if rc != TS_OK:
             self._check(rc)
 

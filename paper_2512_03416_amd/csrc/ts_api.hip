@@ -144,6 +144,12 @@ struct ts_ctx {
     std::vector<Timed> timed;          // recorded, not yet read
     std::vector<hipEvent_t> ev_pool;   // spare events
     int64_t n_alloc = 0;               // device / pinned allocations made so far
+    // Rotary append, tree attention, move, read back: no staging slot, so the ends of their calls are events of their own.
+    static constexpr int kOpEvents = 32;
+    hipEvent_t op_ev[kOpEvents] = {};
+    int op_pos = 0;
+    Rope rope;
+    float* d_tree_o = nullptr; float* d_tree_ml = nullptr;   // partial results of cut scans (kTreePartRows rows)
     uint64_t k_launches[TS_K_COUNT] = {};
     double k_ms[TS_K_COUNT] = {};
 };
@@ -714,6 +720,9 @@ extern "C" int ts_destroy(ts_ctx* c)
     if (c->d_pf_part_ml) (void)hipFree(c->d_pf_part_ml);
     if (c->d_wide_k) (void)hipFree(c->d_wide_k);
     if (c->d_wide_v) (void)hipFree(c->d_wide_v);
+    if (c->d_tree_o) (void)hipFree(c->d_tree_o);
+    if (c->d_tree_ml) (void)hipFree(c->d_tree_ml);
+    for (hipEvent_t e : c->op_ev) if (e) (void)hipEventDestroy(e);
     if (c->side) (void)hipStreamDestroy(c->side);
     for (hipStream_t s : c->parked) (void)hipStreamDestroy(s);
     if (c->h_probe) (void)hipHostFree(c->h_probe);
@@ -1185,4 +1194,391 @@ extern "C" int ts_kernel_times(ts_ctx* c, ts_kernel_stats* out, int reset)
         if (reset) { c->k_launches[k] = 0; c->k_ms[k] = 0.0; }
     }
     return TS_OK;
+}
+
+// ---- rotary append, tree attention, move, read back ---------------------------------------------------
+
+namespace {
+
+// A call of these entry points: they have no work lists in memory, so all that is left of a pass's bookkeeping is the order
+// among streams.  A call that is being captured neither waits for earlier calls nor is waited for (see tokenscale.h).
+struct Op {
+    ts_ctx* c; hipStream_t st;
+    bool eager = false;
+    hipEvent_t end = nullptr;                              // marks the end of an eager call, on its last kernel
+    int begin()
+    {
+        eager = events_on_kernels(st);
+        c->timing_now = eager && c->timing > 0 && (c->timing_pass++ % (uint64_t)c->timing) == 0;
+        if (!eager) return TS_OK;
+        if (c->have_work && st != c->last_stream) {
+            TS_HIP(c, hipStreamWaitEvent(st, c->last_event, 0));
+            if (c->last_side_event) TS_HIP(c, hipStreamWaitEvent(st, c->last_side_event, 0));
+        }
+        hipEvent_t& e = c->op_ev[c->op_pos];
+        c->op_pos = (c->op_pos + 1) % ts_ctx::kOpEvents;
+        if (!e) TS_HIP(c, hipEventCreateWithFlags(&e, hipEventDisableTiming | hipEventDisableSystemFence));
+        else TS_HIP(c, hipEventSynchronize(e));            // (of the call before the last 31: as a rule long past)
+        end = e;
+        return TS_OK;
+    }
+    // After the last launch.  marked: it carried the event.
+    int finish(bool marked)
+    {
+        if (!eager) return TS_OK;
+        c->last_stream = st;
+        c->have_work = true;
+        c->last_event = end;
+        c->last_side_event = nullptr;
+        if (!marked) TS_HIP(c, hipEventRecord(end, st));
+        return TS_OK;
+    }
+};
+
+// A call that fails between two launches: what was launched is marked all the same.
+struct OpGuard {
+    Op& op; bool done = false;
+    ~OpGuard() { if (!done) (void)op.finish(false); }
+};
+
+// Option "validate_block_table" for these calls: pages(i) = pages that sequence i uses.
+template <typename F>
+int check_op_pages(Op& op, const int32_t* block_table, int num_seqs, F&& pages)
+{
+    ts_ctx* c = op.c;
+    if (!c->validate_pages || num_seqs <= 0) return TS_OK;
+    if (!op.eager) return fail(c, TS_ERR_UNSUPPORTED, "the validate_block_table option waits for the GPU: not available under capture");
+    int32_t* res = c->d_q_ctr + 120;                       // (the words of check_pages)
+    TS_HIP(c, hipMemsetAsync(res, 0, 4 * sizeof(int32_t), op.st));
+    for (int s0 = 0; s0 < num_seqs; s0 += kPageCheckSeqs) {
+        PageCheck p{};
+        p.n = std::min(kPageCheckSeqs, num_seqs - s0);
+        p.first = s0;
+        for (int i = 0; i < p.n; ++i) p.pages[i] = pages(s0 + i);
+        TS_HIP(c, (hipError_t)launch_check_pages(p, block_table, c->desc.max_pages_per_seq, c->desc.num_pages, res, op.st));
+    }
+    int32_t host[4] = {0, 0, 0, 0};
+    TS_HIP(c, hipMemcpyAsync(host, res, sizeof host, hipMemcpyDeviceToHost, op.st));
+    TS_HIP(c, hipStreamSynchronize(op.st));
+    if (host[0] != 0)
+        return fail(c, TS_ERR_INVALID_ARG, "block_table: " + std::to_string(host[0]) + " page id(s) outside [0, num_pages), e.g. sequence " +
+                                               std::to_string(host[1]) + ", page " + std::to_string(host[2]));
+    return TS_OK;
+}
+
+// Nothing that is thrown (the host's memory may run out) leaves a C entry point.
+template <typename F>
+int guarded(ts_ctx* c, F&& body)
+{
+    try {
+        return body();
+    } catch (const std::bad_alloc&) {
+        return fail(c, TS_ERR_NOMEM, "out of host memory");
+    }
+}
+
+// The sequences [s0, s0 + n) as kernel arguments; returns the pages that their tokens touch.
+int64_t op_seqs(AppendSeqs* out, const int32_t* lens, const int32_t* prefixes, int64_t row0, int s0, int n)
+{
+    out->n = n; out->pad0 = out->pad1 = 0;
+    int64_t units = 0, row = row0;
+    for (int i = 0; i < n; ++i) {
+        const int32_t prefix = prefixes ? prefixes[s0 + i] : 0, len = lens[s0 + i];
+        out->seq[i] = AppendSeq{(int32_t)row, prefix, (int32_t)units};
+        if (len > 0) units += (prefix + len - 1) / kPage - prefix / kPage + 1;
+        row += len;
+    }
+    out->seq[n] = AppendSeq{(int32_t)row, 0, (int32_t)units};
+    out->n_pages = (int32_t)units;
+    return units;
+}
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+}  // namespace
+
+extern "C" int ts_set_rope(ts_ctx* c, const ts_rope_desc* rope)
+{
+    if (!c) return TS_ERR_INVALID_ARG;
+    return guarded(c, [&]() -> int {
+        c->err.clear();
+        if (!rope) { c->rope = Rope{}; return TS_OK; }
+        double freq[kMaxPairs], scale = 1.0;
+        const int rc = rope_frequencies(rope, freq, &scale, &c->err);
+        if (rc != TS_OK) return rc;
+        if (rope->rot_dim > c->desc.head_dim) return fail(c, TS_ERR_INVALID_ARG, "rot_dim exceeds head_dim");
+        Rope r;
+        r.rot_dim = rope->rot_dim;
+        r.interleaved = rope->layout == TS_ROPE_INTERLEAVED;
+        r.scale = (float)scale;
+        for (int i = 0; i < rope->rot_dim / 2; ++i) r.turns[i] = freq[i] / 6.283185307179586476925;
+        c->rope = r;
+        return TS_OK;
+    });
+}
+
+extern "C" int ts_rope_kv_append(ts_ctx* c, void* stream, const void* q, int64_t q_stride, const void* k_new, int64_t k_stride,
+                                 const void* v_new, int64_t v_stride, void* q_out, void* k_cache, void* v_cache, const float* k_scale,
+                                 const float* v_scale, const int32_t* block_table, const int32_t* positions, const int32_t* q_lens,
+                                 const int32_t* ctx_lens, int num_seqs)
+{
+    if (!c) return TS_ERR_INVALID_ARG;
+    return guarded(c, [&]() -> int {
+        c->err.clear();
+        int rc = check_common(c, k_cache, v_cache, k_scale, v_scale, block_table, q_lens, ctx_lens, num_seqs);
+        if (rc != TS_OK) return rc;
+        if (c->rope.rot_dim == 0) return fail(c, TS_ERR_INVALID_ARG, "no rotary positions set (ts_set_rope)");
+        const int64_t qw = (int64_t)c->desc.num_q_heads * c->desc.head_dim, kw = (int64_t)c->desc.num_kv_heads * c->desc.head_dim;
+        if ((q_stride != 0 && q_stride < qw) || (k_stride != 0 && k_stride < kw) || (v_stride != 0 && v_stride < kw))
+            return fail(c, TS_ERR_INVALID_ARG, "a stride is smaller than a token's row");
+        if ((q == nullptr) != (q_out == nullptr)) return fail(c, TS_ERR_INVALID_ARG, "q and q_out must both be given or both be NULL");
+        if (q && q == q_out && q_stride != 0 && q_stride != qw) return fail(c, TS_ERR_INVALID_ARG, "q_out may be q only if its rows are packed");
+        int64_t total = 0;
+        for (int s = 0; s < num_seqs; ++s) total += q_lens[s];
+        if (total == 0) return TS_OK;
+        if (!k_new || !v_new) return fail(c, TS_ERR_INVALID_ARG, "k_new / v_new is NULL");
+        DeviceGuard guard(c->device);
+        Op op{c, (hipStream_t)stream};
+        rc = op.begin();
+        if (rc != TS_OK) return rc;
+        rc = check_op_pages(op, block_table, num_seqs, [&](int s) { return (ctx_lens[s] + kPage - 1) / kPage; });
+        if (rc != TS_OK) return rc;
+        RopeArgs a{};
+        a.geo = geometry_of(c->desc);
+        a.q = q; a.k = k_new; a.v = v_new; a.q_out = q_out;
+        a.q_stride = q_stride ? q_stride : qw; a.k_stride = k_stride ? k_stride : kw; a.v_stride = v_stride ? v_stride : kw;
+        a.k_cache = k_cache; a.v_cache = v_cache; a.k_scale = k_scale; a.v_scale = v_scale;
+        a.positions = positions;
+        a.rope = c->rope;
+        const int64_t es = c->desc.q_dtype == TS_F32 ? 4 : 2;
+        a.vectors = aligned16(q) && aligned16(q_out) && aligned16(k_new) && aligned16(v_new) &&
+                    (a.q_stride * es) % 16 == 0 && (a.k_stride * es) % 16 == 0 && (a.v_stride * es) % 16 == 0;
+        std::vector<int32_t> prefix((size_t)num_seqs);
+        for (int s = 0; s < num_seqs; ++s) prefix[s] = ctx_lens[s] - q_lens[s];
+        int last = -1;                                     // the last launch that has work carries the event
+        for (int s = 0; s < num_seqs; ++s) if (q_lens[s] > 0) last = s;
+        OpGuard og{op};
+        int64_t row = 0;
+        for (int s0 = 0; s0 <= last; s0 += kAppendSeqs) {
+            AppendSeqs seqs;
+            const int n = std::min(kAppendSeqs, num_seqs - s0);
+            const int64_t units = op_seqs(&seqs, q_lens, prefix.data(), row, s0, n);
+            row = seqs.seq[n].row0;
+            if (units == 0) continue;
+            a.block_table = block_table + (int64_t)s0 * c->desc.max_pages_per_seq;
+            a.heads_per_slice = rope_heads_per_slice(c->desc, units, c->opt.n_cu);
+            a.q_slices = q ? (c->desc.num_q_heads + a.heads_per_slice - 1) / a.heads_per_slice : 0;
+            const hipEvent_t done = last < s0 + n ? op.end : nullptr;
+            const hipError_t e = (hipError_t)timed_launch(c, TS_K_APPEND, true, op.st, [&] { return launch_rope_append(a, seqs, (int32_t)units, stream, done); });
+            if (e != hipSuccess) return hip_fail(c, e, "rotary append launch");
+        }
+        og.done = true;
+        return op.finish(op.end != nullptr);
+    });
+}
+
+extern "C" int ts_reserve_tree(ts_ctx* c)
+{
+    if (!c) return TS_ERR_INVALID_ARG;
+    c->err.clear();
+    if (c->d_tree_o) return TS_OK;
+    DeviceGuard guard(c->device);
+    if (hipMalloc((void**)&c->d_tree_ml, (size_t)kTreePartRows * 2 * sizeof(float)) != hipSuccess ||
+        hipMalloc((void**)&c->d_tree_o, (size_t)kTreePartRows * c->desc.head_dim * sizeof(float)) != hipSuccess) {
+        (void)hipGetLastError();
+        if (c->d_tree_ml) (void)hipFree(c->d_tree_ml);
+        c->d_tree_ml = c->d_tree_o = nullptr;
+        return fail(c, TS_ERR_NOMEM, "scratch of the tree attention could not be allocated");
+    }
+    c->n_alloc += 2;
+    return TS_OK;
+}
+
+extern "C" int ts_tree_attention(ts_ctx* c, void* stream, const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
+                                 const float* v_scale, const int32_t* block_table, const uint64_t* tree_mask, int mask_words,
+                                 const int32_t* q_lens, const int32_t* ctx_lens, int num_seqs, float sm_scale, void* out)
+{
+    if (!c) return TS_ERR_INVALID_ARG;
+    return guarded(c, [&]() -> int {
+        c->err.clear();
+        int rc = check_common(c, k_cache, v_cache, k_scale, v_scale, block_table, q_lens, ctx_lens, num_seqs);
+        if (rc != TS_OK) return rc;
+        if (!(sm_scale == sm_scale)) return fail(c, TS_ERR_INVALID_ARG, "sm_scale is NaN");
+        int64_t total = 0;
+        for (int s = 0; s < num_seqs; ++s) {
+            if (q_lens[s] > TS_TREE_MAX_NODES)
+                return fail(c, TS_ERR_UNSUPPORTED, "sequence " + std::to_string(s) + ": " + std::to_string(q_lens[s]) + " nodes, at most " +
+                                                       std::to_string(TS_TREE_MAX_NODES));
+            if (tree_mask && (mask_words < 1 || (int64_t)mask_words * 64 < q_lens[s]))
+                return fail(c, TS_ERR_INVALID_ARG, "sequence " + std::to_string(s) + ": " + std::to_string(q_lens[s]) + " nodes need more than " +
+                                                       std::to_string(mask_words) + " mask words");
+            total += q_lens[s];
+        }
+        if (total == 0) return TS_OK;
+        if (!q || !out) return fail(c, TS_ERR_INVALID_ARG, "q / out is NULL");
+        if (!aligned16(q) || !aligned16(out)) return fail(c, TS_ERR_INVALID_ARG, "q / out is not 16-byte aligned");
+        DeviceGuard guard(c->device);
+        const TreePlan plan = plan_tree(c->desc, q_lens, ctx_lens, num_seqs, c->opt.n_cu);
+        Op op{c, (hipStream_t)stream};
+        rc = op.begin();
+        if (rc != TS_OK) return rc;
+        if (plan.part_rows > 0 && !c->d_tree_o) {
+            if (!op.eager) return fail(c, TS_ERR_UNSUPPORTED, "scratch cannot be allocated under capture: call ts_reserve_tree first");
+            rc = ts_reserve_tree(c);
+            if (rc != TS_OK) return rc;
+        }
+        rc = check_op_pages(op, block_table, num_seqs, [&](int s) { return q_lens[s] > 0 ? (ctx_lens[s] + kPage - 1) / kPage : 0; });
+        if (rc != TS_OK) return rc;
+        TreeArgs a{};
+        a.geo = geometry_of(c->desc);
+        a.q = q; a.k_cache = k_cache; a.v_cache = v_cache; a.k_scale = k_scale; a.v_scale = v_scale;
+        a.mask = tree_mask; a.mask_words = tree_mask ? mask_words : 0;
+        a.sm_scale = sm_scale > 0.0f ? sm_scale : 1.0f / sqrtf((float)c->desc.head_dim);
+        a.out = out;
+        a.part_pages = plan.part_pages; a.rows = plan.rows;
+        a.part_o = c->d_tree_o; a.part_ml = c->d_tree_ml;
+        int last = -1;
+        for (int s = 0; s < num_seqs; ++s) if (q_lens[s] > 0) last = s;
+        OpGuard og{op};
+        int64_t row = 0, part_row = 0;
+        bool marked = false;
+        for (int s0 = 0; s0 <= last;) {
+            TreeSeqs seqs;
+            int64_t items = 0, merge = 0;
+            int n = 0;
+            for (; n < kTreeSeqs && s0 + n < num_seqs; ++n) {
+                const int32_t len = q_lens[s0 + n];
+                const int32_t parts = len > 0 ? tree_parts(ctx_lens[s0 + n], plan.part_pages) : 0;
+                const int64_t more = (int64_t)parts * c->desc.num_kv_heads * tree_groups(len, a.geo.G, plan.rows);
+                if (n > 0 && items + more > kMaxWorkgroups) break;
+                seqs.seq[n] = TreeSeq{(int32_t)row, ctx_lens[s0 + n] - len, (int32_t)items, parts, (int32_t)merge, (int32_t)part_row};
+                row += len;
+                items += more;
+                if (parts > 1) {
+                    merge += (int64_t)len * c->desc.num_q_heads;
+                    part_row += (int64_t)parts * len * c->desc.num_q_heads;
+                }
+            }
+            seqs.n = n; seqs.pad = 0;
+            seqs.seq[n] = TreeSeq{(int32_t)row, 0, (int32_t)items, 0, (int32_t)merge, (int32_t)part_row};
+            a.block_table = block_table + (int64_t)s0 * c->desc.max_pages_per_seq;
+            s0 += n;
+            if (items == 0) continue;
+            const hipEvent_t done = s0 > last ? op.end : nullptr;
+            hipError_t e = (hipError_t)timed_launch(c, TS_K_DECODE, true, op.st, [&] { return launch_tree(a, seqs, items, stream, merge > 0 ? nullptr : done); });
+            if (e != hipSuccess) return hip_fail(c, e, "tree attention launch");
+            e = (hipError_t)timed_launch(c, TS_K_COMBINE, merge > 0, op.st, [&] { return launch_tree_merge(a, seqs, (int32_t)merge, stream, done); });
+            if (e != hipSuccess) return hip_fail(c, e, "tree merge launch");
+            marked = done != nullptr;
+        }
+        og.done = true;
+        return op.finish(marked);
+    });
+}
+
+extern "C" int ts_kv_move(ts_ctx* c, void* stream, void* k_cache, void* v_cache, const int32_t* block_table, const int32_t* src,
+                          const int32_t* dst, const int32_t* move_lens, const int32_t* ctx_lens, int num_seqs)
+{
+    if (!c) return TS_ERR_INVALID_ARG;
+    return guarded(c, [&]() -> int {
+        c->err.clear();
+        if (num_seqs < 0) return fail(c, TS_ERR_INVALID_ARG, "num_seqs is negative");
+        if (!k_cache || !v_cache) return fail(c, TS_ERR_INVALID_ARG, "k_cache / v_cache is NULL");
+        if (num_seqs > 0 && (!block_table || !move_lens || !ctx_lens)) return fail(c, TS_ERR_INVALID_ARG, "block_table / move_lens / ctx_lens is NULL");
+        int64_t total = 0;
+        int last = -1;
+        for (int s = 0; s < num_seqs; ++s) {
+            if (move_lens[s] < 0 || ctx_lens[s] < 0) return fail(c, TS_ERR_INVALID_ARG, "sequence " + std::to_string(s) + ": negative length");
+            if ((int64_t)ctx_lens[s] > (int64_t)kPage * c->desc.max_pages_per_seq)
+                return fail(c, TS_ERR_INVALID_ARG, "sequence " + std::to_string(s) + ": ctx_len exceeds 16 * max_pages_per_seq");
+            if (move_lens[s] > TS_MAX_MOVES)
+                return fail(c, TS_ERR_UNSUPPORTED, "sequence " + std::to_string(s) + ": more than " + std::to_string(TS_MAX_MOVES) + " moves");
+            total += move_lens[s];
+            if (move_lens[s] > 0) last = s;
+        }
+        if (total == 0) return TS_OK;
+        if (total >= (int64_t)1 << 31) return fail(c, TS_ERR_INVALID_ARG, "too many moves");
+        if (!src || !dst) return fail(c, TS_ERR_INVALID_ARG, "src / dst is NULL");
+        DeviceGuard guard(c->device);
+        Op op{c, (hipStream_t)stream};
+        int rc = op.begin();
+        if (rc != TS_OK) return rc;
+        rc = check_op_pages(op, block_table, num_seqs, [&](int s) { return move_lens[s] > 0 ? (ctx_lens[s] + kPage - 1) / kPage : 0; });
+        if (rc != TS_OK) return rc;
+        MoveArgs a{};
+        a.geo = geometry_of(c->desc);
+        a.k_cache = k_cache; a.v_cache = v_cache; a.src = src; a.dst = dst;
+        OpGuard og{op};
+        int64_t first = 0;
+        const int most = (int)std::min<int64_t>(kMoveSeqs, std::max<int64_t>(1, kMaxWorkgroups / c->desc.num_kv_heads));
+        for (int s0 = 0; s0 <= last; s0 += most) {
+            MoveSeqs seqs{};
+            seqs.n = std::min(most, last + 1 - s0);
+            const int64_t before = first;
+            for (int i = 0; i < seqs.n; ++i) {
+                seqs.first[i] = (int32_t)first;
+                seqs.ctx_len[i] = ctx_lens[s0 + i];
+                first += move_lens[s0 + i];
+            }
+            seqs.first[seqs.n] = (int32_t)first;
+            if (first == before) continue;
+            a.block_table = block_table + (int64_t)s0 * c->desc.max_pages_per_seq;
+            const hipEvent_t done = last < s0 + seqs.n ? op.end : nullptr;
+            const hipError_t e = (hipError_t)timed_launch(c, TS_K_APPEND, true, op.st, [&] { return launch_kv_move(a, seqs, stream, done); });
+            if (e != hipSuccess) return hip_fail(c, e, "move launch");
+        }
+        og.done = true;
+        return op.finish(op.end != nullptr);
+    });
+}
+
+extern "C" int ts_kv_read(ts_ctx* c, void* stream, const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                          const int32_t* block_table, const int32_t* starts, const int32_t* lens, int num_seqs, void* k_out, void* v_out)
+{
+    if (!c) return TS_ERR_INVALID_ARG;
+    return guarded(c, [&]() -> int {
+        c->err.clear();
+        if (num_seqs < 0) return fail(c, TS_ERR_INVALID_ARG, "num_seqs is negative");
+        if (!k_cache || !v_cache) return fail(c, TS_ERR_INVALID_ARG, "k_cache / v_cache is NULL");
+        if (c->desc.kv_dtype == TS_FP8_E4M3 && (!k_scale || !v_scale)) return fail(c, TS_ERR_INVALID_ARG, "fp8 cache needs k_scale and v_scale");
+        if (num_seqs > 0 && (!block_table || !lens)) return fail(c, TS_ERR_INVALID_ARG, "block_table / lens is NULL");
+        int64_t total = 0;
+        int last = -1;
+        for (int s = 0; s < num_seqs; ++s) {
+            if (lens[s] < 0 || (starts && starts[s] < 0)) return fail(c, TS_ERR_INVALID_ARG, "sequence " + std::to_string(s) + ": negative start or length");
+            if ((starts ? (int64_t)starts[s] : 0) + lens[s] > std::min((int64_t)kPage * c->desc.max_pages_per_seq, (int64_t)INT32_MAX))
+                return fail(c, TS_ERR_INVALID_ARG, "sequence " + std::to_string(s) + ": positions beyond 16 * max_pages_per_seq");
+            total += lens[s];
+            if (lens[s] > 0) last = s;
+        }
+        if (total == 0) return TS_OK;
+        if (total >= (int64_t)1 << 31) return fail(c, TS_ERR_INVALID_ARG, "too many tokens");
+        if (!k_out && !v_out) return fail(c, TS_ERR_INVALID_ARG, "k_out and v_out are NULL");
+        DeviceGuard guard(c->device);
+        Op op{c, (hipStream_t)stream};
+        int rc = op.begin();
+        if (rc != TS_OK) return rc;
+        rc = check_op_pages(op, block_table, num_seqs, [&](int s) { return lens[s] > 0 ? (int32_t)(((starts ? (int64_t)starts[s] : 0) + lens[s] + kPage - 1) / kPage) : 0; });
+        if (rc != TS_OK) return rc;
+        ReadArgs a{};
+        a.geo = geometry_of(c->desc);
+        a.k_cache = k_cache; a.v_cache = v_cache; a.k_scale = k_scale; a.v_scale = v_scale;
+        a.k_out = k_out; a.v_out = v_out;
+        a.vectors = aligned16(k_out) && aligned16(v_out);
+        OpGuard og{op};
+        int64_t row = 0;
+        for (int s0 = 0; s0 <= last; s0 += kAppendSeqs) {
+            AppendSeqs seqs;
+            const int n = std::min(kAppendSeqs, num_seqs - s0);
+            const int64_t units = op_seqs(&seqs, lens, starts, row, s0, n);
+            row = seqs.seq[n].row0;
+            if (units == 0) continue;
+            a.block_table = block_table + (int64_t)s0 * c->desc.max_pages_per_seq;
+            const hipEvent_t done = last < s0 + n ? op.end : nullptr;
+            const hipError_t e = (hipError_t)timed_launch(c, TS_K_APPEND, true, op.st, [&] { return launch_kv_read(a, seqs, (int32_t)units, stream, done); });
+            if (e != hipSuccess) return hip_fail(c, e, "read launch");
+        }
+        og.done = true;
+        return op.finish(op.end != nullptr);
+    });
 }

@@ -283,6 +283,115 @@ struct SmallLists {
 
 static_assert(sizeof(AttnArgs) + sizeof(SmallLists) <= 4096 && sizeof(AppendArgs) + sizeof(AppendSeqs) <= 4096, "kernel arguments");
 
+// ---- rotary append, move, read back ------------------------------------------------------------
+
+constexpr int kMaxPairs = 64;          // pairs of a head of 128 dims
+// Angle per position in turns, in double precision (a position of 10^5 has to keep its place within a turn), pairs beyond
+// the rotated dims 0; 0.5 KB of the kernel arguments.
+struct Rope {
+    int32_t rot_dim = 0;               // 0 = none set
+    int32_t interleaved = 0;
+    float scale = 1.0f;
+    double turns[kMaxPairs] = {};
+};
+
+// A launch covers the pages [first_unit, first_unit + units) that its sequences' new tokens (or the tokens to read) touch.
+struct RopeArgs {
+    Geometry geo;
+    const void* q; const void* k; const void* v;
+    int64_t q_stride, k_stride, v_stride;      // elements from token row to token row
+    void* q_out;
+    void* k_cache; void* v_cache;
+    const float* k_scale; const float* v_scale;
+    const int32_t* block_table;        // of the launch's first sequence
+    const int32_t* positions;
+    int32_t q_slices;                  // workgroups that share a page's query heads
+    int32_t heads_per_slice;
+    int32_t vectors;                   // bases and strides are multiples of 16 bytes
+    int32_t first_unit;
+    Rope rope;
+};
+static_assert(sizeof(RopeArgs) + sizeof(AppendSeqs) <= 4096, "kernel arguments");
+
+struct MoveArgs {
+    Geometry geo;
+    void* k_cache; void* v_cache;
+    const int32_t* block_table;        // of the launch's first sequence
+    const int32_t* src; const int32_t* dst;
+};
+struct MoveSeqs {                      // sequence i's pairs are [first[i], first[i + 1])
+    int32_t n, pad;
+    int32_t first[257];
+    int32_t ctx_len[256];
+};
+constexpr int kMoveSeqs = 256;
+
+struct ReadArgs {
+    Geometry geo;
+    const void* k_cache; const void* v_cache;
+    const float* k_scale; const float* v_scale;
+    const int32_t* block_table;        // of the launch's first sequence
+    void* k_out; void* v_out;
+    int32_t vectors;                   // outputs are 16-byte aligned
+    int32_t first_unit;
+};
+
+struct PageCheck { int32_t n, first; int32_t pages[512]; };     // pages that sequence first + i uses
+constexpr int kPageCheckSeqs = 512;
+
+// ---- attention of drafted trees ----------------------------------------------------------------
+
+// A sequence's work: `parts` ranges of `part_pages` pages, `groups` groups of rows, every KV head.  Row r of a KV head is
+// (node r / G, head r % G of the group).
+struct TreeSeq {
+    int32_t row0;                      // first node's row; the next entry's row0 ends the sequence
+    int32_t prefix;
+    int32_t first_item;                // workgroups of the sequences before it
+    int32_t parts;                     // key ranges the scan is cut into
+    int32_t first_merge;               // rows to merge (over KV heads) of the sequences before it in this launch
+    int32_t part_row0;                 // first partial row (parts > 1)
+};
+constexpr int kTreeSeqs = 128;         // 3 KB of the 4 KB of kernel arguments
+struct TreeSeqs {
+    int32_t n, pad;
+    TreeSeq seq[kTreeSeqs + 1];
+};
+struct TreeArgs {
+    Geometry geo;
+    const void* q;
+    const void* k_cache; const void* v_cache;
+    const float* k_scale; const float* v_scale;
+    const int32_t* block_table;        // of the launch's first sequence
+    const uint64_t* mask; int32_t mask_words;
+    float sm_scale;
+    void* out;
+    int32_t part_pages;                // pages of a key range, even
+    int32_t rows;                      // rows of a workgroup
+    float* part_o;                     // [partial row][D] fp32, unnormalised
+    float* part_ml;                    // [partial row][2] = (reference maximum in log2 units, weight sum)
+};
+static_assert(sizeof(TreeArgs) + sizeof(TreeSeqs) <= 4096, "kernel arguments");
+constexpr int64_t kTreePartRows = (int64_t)1 << 18;   // partial rows that the scratch holds
+
+// How a batch of trees is cut.
+struct TreePlan {
+    int32_t rows = 0;                  // rows of a workgroup
+    int32_t part_pages = 0;
+    int64_t part_rows = 0;             // partial rows in all
+    int64_t items = 0;
+};
+TreePlan plan_tree(const ts_attn_desc& d, const int32_t* q_lens, const int32_t* ctx_lens, int num_seqs, int n_cu);
+inline int32_t tree_groups(int32_t nodes, int32_t G, int32_t rows) { return (int32_t)(((int64_t)nodes * G + rows - 1) / rows); }
+inline int32_t tree_parts(int32_t ctx_len, int32_t part_pages)
+{
+    const int32_t pages = (ctx_len + kPage - 1) / kPage;
+    return (pages + part_pages - 1) / part_pages;
+}
+
+// Query heads that one workgroup of the rotary append takes of a page's tokens.
+int32_t rope_heads_per_slice(const ts_attn_desc& d, int64_t units, int n_cu);
+int rope_frequencies(const ts_rope_desc* r, double* freq, double* scale, std::string* err);
+
 // Launchers (defined in the .hip files).  All return a hipError_t cast to int.  done: a hipEvent_t recorded at the end of
 // the (last) kernel that is launched, or NULL; a launcher without work does not record it.
 int launch_append(const AppendArgs& a, void* stream, void* done);
@@ -300,5 +409,11 @@ int launch_prefill(const AttnArgs& a, void* stream, void* done);
 int launch_mixed(const AttnArgs& a, void* stream, void* done);
 int launch_prefill_resident(const AttnArgs& a, void* stream, void* done);
 int launch_prefill_combine(const AttnArgs& a, void* stream, void* done);
+int launch_rope_append(const RopeArgs& a, const AppendSeqs& s, int32_t units, void* stream, void* done);
+int launch_kv_read(const ReadArgs& a, const AppendSeqs& s, int32_t units, void* stream, void* done);
+int launch_kv_move(const MoveArgs& a, const MoveSeqs& s, void* stream, void* done);
+int launch_check_pages(const PageCheck& p, const int32_t* block_table, int max_pages, int64_t num_pages, int32_t* result, void* stream);
+int launch_tree(const TreeArgs& a, const TreeSeqs& s, int64_t items, void* stream, void* done);
+int launch_tree_merge(const TreeArgs& a, const TreeSeqs& s, int32_t rows, void* stream, void* done);
 
 }  // namespace ts

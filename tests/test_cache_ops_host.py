@@ -1,0 +1,103 @@
+"""Host side of the rotary append and of the tree attention: frequencies, masks, refusals (no GPU)."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+
+import paper_2512_03416_amd as ts
+from cache_ops_ref import pack_bits, random_tree, tree_see
+from paper_2512_03416_amd import binding
+
+
+@pytest.mark.parametrize("rot", [2, 6, 64, 128])
+@pytest.mark.parametrize("base", [10000.0, 5e5])
+def test_frequencies_of_the_plain_scalings(rot, base):
+    i = np.arange(rot // 2)
+    f, m = ts.rope_frequencies(rot, base=base)
+    np.testing.assert_allclose(f, base ** (-2 * i / rot), rtol=1e-14)
+    assert m == 1.0
+    f2, m2 = ts.rope_frequencies(rot, base=base, scaling="linear", factor=4)
+    np.testing.assert_allclose(f2, f / 4, rtol=1e-14)
+    assert m2 == 1.0
+    f3, _ = ts.rope_frequencies(rot, base=base, scaling="ntk", factor=4)
+    if rot > 2:                                            # the slowest pair is slowed by the factor, the fastest not at all
+        assert f3[0] == 1.0 and math.isclose(f3[-1], f[-1] / 4, rel_tol=1e-12)
+    else:
+        assert f3[0] == 1.0
+    f4, m4 = ts.rope_frequencies(rot, table=0.25 + i, attn_scale=1.5)
+    assert np.array_equal(f4, 0.25 + i) and m4 == 1.5
+
+
+def test_frequencies_of_the_ranged_scalings():
+    rot, base, n, factor = 128, 5e5, 8192, 8.0
+    plain, _ = ts.rope_frequencies(rot, base=base)
+    turns = n * plain / (2 * math.pi)
+    f, m = ts.rope_frequencies(rot, base=base, scaling="wavelength", factor=factor, original_length=n)
+    assert m == 1.0
+    np.testing.assert_allclose(f[turns > 4], plain[turns > 4], rtol=1e-14)
+    np.testing.assert_allclose(f[turns < 1], plain[turns < 1] / factor, rtol=1e-14)
+    mid = (turns > 1) & (turns < 4)
+    assert mid.any() and np.all(f[mid] < plain[mid]) and np.all(f[mid] > plain[mid] / factor)
+    f, m = ts.rope_frequencies(rot, base=base, scaling="yarn", factor=factor, original_length=n)
+    assert math.isclose(m, 1 + 0.1 * math.log(factor), rel_tol=1e-14)
+    lo, hi = np.nonzero(turns >= 32)[0][-1], np.nonzero(turns <= 1)[0][0]      # whole pairs on either side of the ramp
+    np.testing.assert_allclose(f[:lo + 1], plain[:lo + 1], rtol=1e-14)
+    np.testing.assert_allclose(f[hi:], plain[hi:] / factor, rtol=1e-14)
+    ratio = f / plain
+    assert np.all(np.diff(ratio) <= 1e-15)
+
+
+@pytest.mark.parametrize("bad", [dict(rot_dim=3), dict(rot_dim=0), dict(rot_dim=130), dict(rot_dim=64, base=1.0),
+                                 dict(rot_dim=64, base=float("inf")), dict(rot_dim=64, scaling="linear", factor=0.5),
+                                 dict(rot_dim=64, scaling="linear", factor=float("nan")),
+                                 dict(rot_dim=64, scaling="yarn", factor=2.0), dict(rot_dim=64, attn_scale=-1.0),
+                                 dict(rot_dim=64, scaling="wavelength", factor=2.0, original_length=4096, low=4.0, high=4.0),
+                                 dict(rot_dim=64, layout=2), dict(rot_dim=64, scaling=6), dict(rot_dim=64, scaling=5),
+                                 dict(rot_dim=4, table=[1.0, float("inf")])])
+def test_frequencies_refuse(bad):
+    with pytest.raises(ts.TokenScaleError) as e:
+        ts.rope_frequencies(**bad)
+    assert e.value.code == binding.TS_ERR_INVALID_ARG
+
+
+def test_rope_description_refuses_unknown_words():
+    for bad in (dict(layout="halves"), dict(scaling="dynamic"), dict(table=[1.0])):
+        with pytest.raises(ValueError):
+            ts.RopeDesc.make(64, **bad)
+
+
+def test_masks_and_depths():
+    rng = np.random.default_rng(3)
+    lens = [1, 0, 17, 64, 65, 200]
+    trees = [random_tree(rng, n, roots=1 + (n > 20)) for n in lens]
+    masks, depths = ts.tree_masks(np.concatenate(trees), lens)
+    assert masks.shape == (sum(lens), 4) and masks.dtype == np.uint64
+    assert np.array_equal(masks, pack_bits([tree_see(t) for t in trees], 4))
+    assert np.array_equal(depths, np.concatenate([tree_see(t).sum(1) - 1 for t in trees]))
+    empty, none = ts.tree_masks([], [])
+    assert empty.shape == (0, 1) and none.shape == (0,)
+
+
+@pytest.mark.parametrize("parents,lens,words", [([0], [1], 1), ([-1, 1], [2], 1), ([-2], [1], 1), ([-1, 5], [2], 1),
+                                                ([-1] * 65, [65], 1)])
+def test_masks_refuse(parents, lens, words):
+    with pytest.raises(ts.TokenScaleError) as e:
+        ts.tree_masks(parents, lens, words)
+    assert e.value.code == binding.TS_ERR_INVALID_ARG
+
+
+def test_masks_refuse_other_counts():
+    with pytest.raises(ValueError):
+        ts.tree_masks([-1, 0], [3])
+
+
+def test_entry_points_refuse_a_missing_context():
+    lib, null, one = ts.load_library(), ctypes.c_void_p(0), np.ones(1, np.int32).tobytes()
+    assert lib.ts_set_rope(null, None) == binding.TS_ERR_INVALID_ARG
+    assert lib.ts_reserve_tree(null) == binding.TS_ERR_INVALID_ARG
+    assert lib.ts_rope_kv_append(null, *[null] * 2, 0, null, 0, null, 0, *[null] * 7, one, one, 1) == binding.TS_ERR_INVALID_ARG
+    assert lib.ts_tree_attention(null, *[null] * 8, 1, one, one, 1, 0.0, null) == binding.TS_ERR_INVALID_ARG
+    assert lib.ts_kv_move(null, *[null] * 6, one, one, 1) == binding.TS_ERR_INVALID_ARG
+    assert lib.ts_kv_read(null, *[null] * 6, one, one, 1, null, null) == binding.TS_ERR_INVALID_ARG
+    assert lib.ts_rope_frequencies(None, null, null) == binding.TS_ERR_INVALID_ARG
