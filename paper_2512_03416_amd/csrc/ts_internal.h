@@ -365,7 +365,7 @@ struct TreeArgs {
     const uint64_t* mask; int32_t mask_words;
     float sm_scale;
     void* out;
-    int32_t part_pages;                // pages of a key range, even
+    int32_t part_pages;                // pages of a key range, a multiple of 8
     int32_t rows;                      // rows of a workgroup
     float* part_o;                     // [partial row][D] fp32, unnormalised
     float* part_ml;                    // [partial row][2] = (reference maximum in log2 units, weight sum)

@@ -83,8 +83,7 @@ TreePlan plan_tree(const ts_attn_desc& d, const int32_t* q_lens, const int32_t* 
     int32_t longest = 0;
     for (int s = 0; s < num_seqs; ++s)
         if (q_lens[s] > 0) { most = std::max<int64_t>(most, (int64_t)q_lens[s] * G); longest = std::max(longest, ctx_lens[s]); }
-    const int32_t widest = d.q_dtype == TS_F32 ? 32 : 64;
-    p.rows = most <= 16 ? 16 : (most <= 32 ? 32 : widest);
+    p.rows = most <= 32 && d.q_dtype != TS_F32 ? 32 : (most <= 64 ? 64 : 128);
     int64_t pages = 0;                                     // pages read, over the workgroups' groups of rows
     for (int s = 0; s < num_seqs; ++s)
         if (q_lens[s] > 0) pages += (int64_t)tree_groups(q_lens[s], G, p.rows) * ((ctx_lens[s] + kPage - 1) / kPage) * Hkv;
@@ -92,8 +91,8 @@ TreePlan plan_tree(const ts_attn_desc& d, const int32_t* q_lens, const int32_t* 
     int64_t part = std::max<int64_t>(kMinPages, (pages + slots - 1) / slots);
     const int64_t whole = (longest + kPage - 1) / kPage;
     for (;; part *= 2) {
-        part = std::min<int64_t>(part + (part & 1), whole + (whole & 1));
-        p.part_pages = (int32_t)std::max<int64_t>(part, 2);
+        part = std::min<int64_t>((part + 7) / 8 * 8, (whole + 7) / 8 * 8);     // (whole rounds of the waves)
+        p.part_pages = (int32_t)part;
         p.part_rows = p.items = 0;
         for (int s = 0; s < num_seqs; ++s) {
             if (q_lens[s] <= 0) continue;
