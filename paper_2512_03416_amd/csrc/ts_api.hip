@@ -149,6 +149,7 @@ struct ts_ctx {
     hipEvent_t op_ev[kOpEvents] = {};
     int op_pos = 0;
     Rope rope;
+    TreePlan tree_plan;                // (kept for its memory)
     float* d_tree_o = nullptr; float* d_tree_ml = nullptr;   // partial results of cut scans (kTreePartRows rows)
     uint64_t k_launches[TS_K_COUNT] = {};
     double k_ms[TS_K_COUNT] = {};
@@ -1418,7 +1419,9 @@ extern "C" int ts_tree_attention(ts_ctx* c, void* stream, const void* q, const v
         if (!q || !out) return fail(c, TS_ERR_INVALID_ARG, "q / out is NULL");
         if (!aligned16(q) || !aligned16(out)) return fail(c, TS_ERR_INVALID_ARG, "q / out is not 16-byte aligned");
         DeviceGuard guard(c->device);
-        const TreePlan plan = plan_tree(c->desc, q_lens, ctx_lens, num_seqs, c->opt.n_cu);
+        TreePlan& plan = c->tree_plan;
+        plan_tree(c->desc, q_lens, ctx_lens, num_seqs, c->opt.n_cu, &plan);
+        if (plan.part_rows > kTreePartRows) return fail(c, TS_ERR_UNSUPPORTED, "the scratch does not hold the batch's partial results");   // (plan_tree keeps within it)
         Op op{c, (hipStream_t)stream};
         rc = op.begin();
         if (rc != TS_OK) return rc;
@@ -1435,36 +1438,30 @@ extern "C" int ts_tree_attention(ts_ctx* c, void* stream, const void* q, const v
         a.mask = tree_mask; a.mask_words = tree_mask ? mask_words : 0;
         a.sm_scale = sm_scale > 0.0f ? sm_scale : 1.0f / sqrtf((float)c->desc.head_dim);
         a.out = out;
-        a.part_pages = plan.part_pages; a.rows = plan.rows;
+        a.block_table = block_table;
+        a.rows = plan.rows;
         a.part_o = c->d_tree_o; a.part_ml = c->d_tree_ml;
-        int last = -1;
-        for (int s = 0; s < num_seqs; ++s) if (q_lens[s] > 0) last = s;
         OpGuard og{op};
-        int64_t row = 0, part_row = 0;
         bool marked = false;
-        for (int s0 = 0; s0 <= last;) {
+        const size_t n_seqs = plan.seqs.size();
+        for (size_t s0 = 0; s0 < n_seqs;) {
             TreeSeqs seqs;
             int64_t items = 0, merge = 0;
             int n = 0;
-            for (; n < kTreeSeqs && s0 + n < num_seqs; ++n) {
-                const int32_t len = q_lens[s0 + n];
-                const int32_t parts = len > 0 ? tree_parts(ctx_lens[s0 + n], plan.part_pages) : 0;
-                const int64_t more = (int64_t)parts * c->desc.num_kv_heads * tree_groups(len, a.geo.G, plan.rows);
+            for (; n < kTreeSeqs && s0 + n < n_seqs; ++n) {
+                TreeSeq t = plan.seqs[s0 + n];
+                const int64_t more = (int64_t)t.parts * c->desc.num_kv_heads * tree_groups(t.n_nodes, a.geo.G, plan.rows);
                 if (n > 0 && items + more > kMaxWorkgroups) break;
-                seqs.seq[n] = TreeSeq{(int32_t)row, ctx_lens[s0 + n] - len, (int32_t)items, parts, (int32_t)merge, (int32_t)part_row};
-                row += len;
+                t.first_item = (int32_t)items;
+                t.first_merge = (int32_t)merge;
+                seqs.seq[n] = t;
                 items += more;
-                if (parts > 1) {
-                    merge += (int64_t)len * c->desc.num_q_heads;
-                    part_row += (int64_t)parts * len * c->desc.num_q_heads;
-                }
+                if (t.parts > 1) merge += (int64_t)t.n_nodes * c->desc.num_q_heads;
             }
             seqs.n = n; seqs.pad = 0;
-            seqs.seq[n] = TreeSeq{(int32_t)row, 0, (int32_t)items, 0, (int32_t)merge, (int32_t)part_row};
-            a.block_table = block_table + (int64_t)s0 * c->desc.max_pages_per_seq;
-            s0 += n;
-            if (items == 0) continue;
-            const hipEvent_t done = s0 > last ? op.end : nullptr;
+            for (int i = n; i < kTreeSeqs; ++i) seqs.seq[i] = TreeSeq{};
+            s0 += (size_t)n;
+            const hipEvent_t done = s0 >= n_seqs ? op.end : nullptr;
             hipError_t e = (hipError_t)timed_launch(c, TS_K_DECODE, true, op.st, [&] { return launch_tree(a, seqs, items, stream, merge > 0 ? nullptr : done); });
             if (e != hipSuccess) return hip_fail(c, e, "tree attention launch");
             e = (hipError_t)timed_launch(c, TS_K_COMBINE, merge > 0, op.st, [&] { return launch_tree_merge(a, seqs, (int32_t)merge, stream, done); });

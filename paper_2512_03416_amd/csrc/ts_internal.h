@@ -341,31 +341,33 @@ constexpr int kPageCheckSeqs = 512;
 
 // ---- attention of drafted trees ----------------------------------------------------------------
 
-// A sequence's work: `parts` ranges of `part_pages` pages, `groups` groups of rows, every KV head.  Row r of a KV head is
+// A sequence's work: `parts` ranges of part_pages pages, groups of rows, every KV head.  Row r of a KV head is
 // (node r / G, head r % G of the group).
 struct TreeSeq {
-    int32_t row0;                      // first node's row; the next entry's row0 ends the sequence
+    int32_t seq;                       // row of the page table
+    int32_t row0;                      // first node's row
+    int32_t n_nodes;
     int32_t prefix;
-    int32_t first_item;                // workgroups of the sequences before it
+    int32_t first_item;                // workgroups of the launch's sequences before it
     int32_t parts;                     // key ranges the scan is cut into
-    int32_t first_merge;               // rows to merge (over KV heads) of the sequences before it in this launch
+    int32_t part_pages;                // pages of a range: whole rounds of a workgroup's waves
+    int32_t first_merge;               // rows to merge (over KV heads) of the launch's sequences before it
     int32_t part_row0;                 // first partial row (parts > 1)
 };
-constexpr int kTreeSeqs = 128;         // 3 KB of the 4 KB of kernel arguments
+constexpr int kTreeSeqs = 96;          // 3.4 of the 4 KB of kernel arguments
 struct TreeSeqs {
     int32_t n, pad;
-    TreeSeq seq[kTreeSeqs + 1];
+    TreeSeq seq[kTreeSeqs];
 };
 struct TreeArgs {
     Geometry geo;
     const void* q;
     const void* k_cache; const void* v_cache;
     const float* k_scale; const float* v_scale;
-    const int32_t* block_table;        // of the launch's first sequence
+    const int32_t* block_table;
     const uint64_t* mask; int32_t mask_words;
     float sm_scale;
     void* out;
-    int32_t part_pages;                // pages of a key range, a multiple of 8
     int32_t rows;                      // rows of a workgroup
     float* part_o;                     // [partial row][D] fp32, unnormalised
     float* part_ml;                    // [partial row][2] = (reference maximum in log2 units, weight sum)
@@ -373,20 +375,18 @@ struct TreeArgs {
 static_assert(sizeof(TreeArgs) + sizeof(TreeSeqs) <= 4096, "kernel arguments");
 constexpr int64_t kTreePartRows = (int64_t)1 << 18;   // partial rows that the scratch holds
 
-// How a batch of trees is cut.
+// How a batch of trees is cut: its sequences with nodes, longest ranges first (first_item and first_merge are left to the launches).
 struct TreePlan {
     int32_t rows = 0;                  // rows of a workgroup
-    int32_t part_pages = 0;
     int64_t part_rows = 0;             // partial rows in all
-    int64_t items = 0;
+    std::vector<TreeSeq> seqs;
 };
-TreePlan plan_tree(const ts_attn_desc& d, const int32_t* q_lens, const int32_t* ctx_lens, int num_seqs, int n_cu);
+void plan_tree(const ts_attn_desc& d, const int32_t* q_lens, const int32_t* ctx_lens, int num_seqs, int n_cu, TreePlan* plan);
 inline int32_t tree_groups(int32_t nodes, int32_t G, int32_t rows) { return (int32_t)(((int64_t)nodes * G + rows - 1) / rows); }
-inline int32_t tree_parts(int32_t ctx_len, int32_t part_pages)
-{
-    const int32_t pages = (ctx_len + kPage - 1) / kPage;
-    return (pages + part_pages - 1) / part_pages;
-}
+// LDS that a workgroup of the tree kernel takes: a ring of up to four slots of 32 keys for each of its 4 * 32 / rows groups of waves, in
+// at most 80 of the 160 KB of a CU, but at least two slots.
+constexpr int kTreeWaves = 4;
+constexpr int tree_ring_slots(int slot_bytes) { return 80 * 1024 / slot_bytes < 2 ? 2 : (80 * 1024 / slot_bytes > 4 ? 4 : 80 * 1024 / slot_bytes); }
 
 // Query heads that one workgroup of the rotary append takes of a page's tokens.
 int32_t rope_heads_per_slice(const ts_attn_desc& d, int64_t units, int n_cu);

@@ -2,8 +2,8 @@
 //
 // Every node of a tree sees the sequence's prefix and its own ancestors, so all nodes of a sequence share the scan of the
 // prefix: row (node, head of the group) is a column of S^T = K Q^T, and a workgroup reads K and V once for all its rows.
-//   - Four waves: WR of them side by side over the rows (a wave holds NT blocks of 32 columns), WK = 4 / WR of them taking turns
-//     along the keys.  Up to 32 rows: WR = 1, each wave scans its own keys; 256 rows: WR = 4, NT = 2.
+//   - Four waves of 32 columns: WR of them side by side over the rows, WK = 4 / WR of them taking turns along the keys.  Up to 32
+//     rows: WR = 1, each wave scans its own keys.
 //   - Keys come in steps of 32 (two pages) per wave, copied into a ring of LDS slots by the memory system, in the order in which
 //     the matrix instructions take them: a wave's operand read is always 1 KB in lane order (no bank conflicts), and copies in
 //     flight take no registers.  The WR waves of a key group share the copy.
@@ -12,7 +12,8 @@
 //     packed to bf16 they are the B operands of O^T += V^T P^T as they stand, and the matching A operand is 16 bytes (e4m3: 8)
 //     of a V row.  fp32: the same with the 32x32x2 instruction, one dim of a K piece or one token of a V piece per step.
 //   - The masks are looked at on the pages that hold nodes only.
-// The running maximum is a reference in log2 units that is raised when a score exceeds it by more than 16.
+// The running maximum is a reference in log2 units that is raised only when a step's weights add up to more than 2^16 in some lane:
+// any reference gives the same quotient, and the maximum itself is not needed for as long.
 #include <type_traits>
 
 #include "ts_device.h"
@@ -20,8 +21,8 @@
 
 namespace ts {
 
-constexpr int kTrWaves = 4;
-constexpr float kRaiseTr = 16.0f;
+constexpr int kTrWaves = kTreeWaves;
+constexpr float kBigTr = 65536.0f;
 // Reference maximum of a column that has seen no key: finite, so that differences stay defined.
 constexpr float kNoKeyTr = -3.402823466e38f;
 
@@ -103,35 +104,42 @@ __device__ __forceinline__ void tr_load_q(TrQ<KT, D>& t, const void* q, int64_t 
     }
 }
 
-// S^T of 32 keys for NT blocks of 32 columns.
-template <int NT, typename KT, int D>
-__device__ __forceinline__ void tr_scores(f32x16 (&s)[NT], const unsigned char* lk, const TrQ<KT, D> (&q)[NT], int lane)
+// S^T of 32 keys.  The K pieces come from registers where they fit (16-bit arithmetic), else from LDS one by one.
+template <typename KT, int D> struct TrK {
+    static constexpr int N = sizeof(KT) == 4 ? 1 : TrStep<KT, D>::NK;
+    uint4 piece[N];
+};
+template <typename KT, int D>
+__device__ __forceinline__ void tr_load_k(TrK<KT, D>& k, const unsigned char* lk, int lane)
 {
+    if constexpr (sizeof(KT) != 4) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+        for (int b = 0; b < TrK<KT, D>::N; ++b) k.piece[b] = *(const uint4*)(lk + b * 1024 + lane * 16);
+    }
+}
+template <typename KT, int D>
+__device__ __forceinline__ f32x16 tr_scores(const TrK<KT, D>& k, [[maybe_unused]] const unsigned char* lk, const TrQ<KT, D>& q, [[maybe_unused]] int lane)
+{
+    f32x16 s = {};
+    if constexpr (sizeof(KT) == 4) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
+        for (int b = 0; b < TrStep<KT, D>::NK; ++b) {
+            const f32x4 kf = *(const f32x4*)(lk + b * 1024 + lane * 16);
 #pragma unroll
-    for (int b = 0; b < TrStep<KT, D>::NK; ++b) {
-        const uint4 k = *(const uint4*)(lk + b * 1024 + lane * 16);
-        if constexpr (sizeof(KT) == 4) {
-            const f32x4 kf = __builtin_bit_cast(f32x4, k);
+            for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], q.q[b][e], s, 0, 0, 0);
+        }
+    } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int t = 0; t < NT; ++t) s[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], q[t].q[b][e], s[t], 0, 0, 0);
-        } else if constexpr (sizeof(KT) == 2) {
-#pragma unroll
-            for (int t = 0; t < NT; ++t) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k), q[t].q[b], s[t], 0, 0, 0);
-        } else {
-            const uint2 a0 = tr_widen(k.x), a1 = tr_widen(k.y), a2 = tr_widen(k.z), a3 = tr_widen(k.w);
-            const bf16x8 lo = __builtin_bit_cast(bf16x8, make_uint4(a0.x, a0.y, a1.x, a1.y)), hi = __builtin_bit_cast(bf16x8, make_uint4(a2.x, a2.y, a3.x, a3.y));
-#pragma unroll
-            for (int t = 0; t < NT; ++t) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lo, q[t].q[2 * b], s[t], 0, 0, 0);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(hi, q[t].q[2 * b + 1], s[t], 0, 0, 0);
+        for (int b = 0; b < TrK<KT, D>::N; ++b) {
+            if constexpr (sizeof(KT) == 2) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k.piece[b]), q.q[b], s, 0, 0, 0);
+            else {
+                const uint2 a0 = tr_widen(k.piece[b].x), a1 = tr_widen(k.piece[b].y), a2 = tr_widen(k.piece[b].z), a3 = tr_widen(k.piece[b].w);
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, make_uint4(a0.x, a0.y, a1.x, a1.y)), q.q[2 * b], s, 0, 0, 0);
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, make_uint4(a2.x, a2.y, a3.x, a3.y)), q.q[2 * b + 1], s, 0, 0, 0);
+            }
         }
     }
+    return s;
 }
 
 // A lane's eight tokens (8h ..) of dim 32 d + n of page p, as they lie in LDS: VW words.
@@ -206,17 +214,19 @@ __device__ __forceinline__ uint32_t tr_seen(const TreeArgs& a, int row0, int n_n
 }
 
 // What a workgroup does, from the launch's list.
-struct TrItem { int seq, node_rows, n_nodes, row0, prefix, g, group, part, parts, part_row0; };
+struct TrItem { int seq, node_rows, n_nodes, row0, prefix, g, group, part, parts, part_pages, part_row0; };
 __device__ __forceinline__ TrItem tr_item(const TreeArgs& a, const TreeSeqs& s)
 {
     const int lane = threadIdx.x & 63, w = blockIdx.x;
     int i = -1;
 #pragma unroll
-    for (int b = 0; b < kTreeSeqs; b += 64)
-        i += __builtin_popcountll(__ballot((b + lane < s.n) & (s.seq[b + lane].first_item <= w)));
+    for (int b = 0; b < kTreeSeqs; b += 64) {
+        const int k = min(b + lane, kTreeSeqs - 1);
+        i += __builtin_popcountll(__ballot((b + lane < s.n) & (s.seq[k].first_item <= w)));
+    }
     const TreeSeq q = s.seq[i];
     TrItem t;
-    t.seq = i; t.row0 = q.row0; t.n_nodes = s.seq[i + 1].row0 - q.row0; t.prefix = q.prefix; t.parts = q.parts; t.part_row0 = q.part_row0;
+    t.seq = q.seq; t.row0 = q.row0; t.n_nodes = q.n_nodes; t.prefix = q.prefix; t.parts = q.parts; t.part_pages = q.part_pages; t.part_row0 = q.part_row0;
     t.node_rows = t.n_nodes * a.geo.G;
     // The groups of rows of one scan (KV head, range of pages) read the same pages: they go to the same die, one after the
     // other (workgroup i runs on die i % 8).
@@ -248,29 +258,25 @@ __device__ __forceinline__ float tr_inverse(const TreeArgs& a, float l, int pref
     return inv;
 }
 
-// LDS slots of the ring: two workgroups per CU where at least two slots fit (80 of 160 KB), four at the most.
-template <typename KT, int D, int WR> constexpr int tr_ring()
-{
-    constexpr int slot = TrStep<KT, D>::kBytes * (kTrWaves / WR), fit = 80 * 1024 / slot;
-    return fit < 2 ? 2 : (fit > 4 ? 4 : fit);
-}
+template <typename KT, int D, int WR> constexpr int tr_ring() { return tree_ring_slots(TrStep<KT, D>::kBytes * (kTrWaves / WR)); }
 
-template <typename KT, int D, int WR, int NT>
-__global__ __launch_bounds__(64 * kTrWaves, NT == 1 ? 2 : 1) void tree_kernel(TreeArgs a, TreeSeqs s)
+template <typename KT, int D, int WR>
+__global__ __launch_bounds__(64 * kTrWaves) void tree_kernel(TreeArgs a, TreeSeqs s)
 {
     using S = TrStep<KT, D>;
-    constexpr int WK = kTrWaves / WR, DB = D / 32, ROWS = 32 * WR * NT, R = tr_ring<KT, D, WR>(), C = S::NB / WR;
-    static_assert(S::NB % WR == 0 && C * (R - 2) < 64, "copies per wave");
+    constexpr bool F32 = sizeof(KT) == 4;
+    constexpr int WK = kTrWaves / WR, DB = D / 32, ROWS = 32 * WR, R = tr_ring<KT, D, WR>(), C = S::NB / WR;
+    static_assert(S::NB % WR == 0 && C * (R - 1) < 64, "copies per wave");
     __shared__ __align__(16) unsigned char ring[R][WK][S::kBytes];
-    static_assert(sizeof ring >= (size_t)(kTrWaves - WR) * (NT * DB * 4096 + NT * 256), "the ring holds the waves' states at the end");
+    static_assert(sizeof ring >= (size_t)(kTrWaves - WR) * (DB * 4096 + 256), "the ring holds the waves' states at the end");
     const TrItem it = tr_item(a, s);
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, h = lane >> 5, n = lane & 31;
     const int wr = wave % WR, kg = wave / WR;
     const int Hq = a.geo.Hq, Hkv = a.geo.Hkv, G = a.geo.G;
     const int ctx_len = it.prefix + it.n_nodes, pages = (ctx_len + kPage - 1) / kPage;
-    const int page0 = it.part * a.part_pages, page1 = min(page0 + a.part_pages, pages);
+    const int page0 = it.part * it.part_pages, page1 = min(page0 + it.part_pages, pages);
     const int n_step = (page1 - page0 + 2 * WK - 1) / (2 * WK);
-    const int first_row = it.group * ROWS + wr * (32 * NT);
+    const int first_row = it.group * ROWS + wr * 32;
     const bool works = first_row < it.node_rows;               // (a wave without rows only copies)
 
     const int32_t TS_CONSTANT* bt = as_constant(a.block_table) + (int64_t)it.seq * a.geo.max_pages;
@@ -278,300 +284,309 @@ __global__ __launch_bounds__(64 * kTrWaves, NT == 1 ? 2 : 1) void tree_kernel(Tr
     const char* vc = (const char*)a.v_cache;
     // (past the end of the range: its last page again, whose keys do not count a second time)
     auto page_of = [&](int i) { return page0 + 2 * (WK * i + kg); };
-    auto tile_of = [&](int page) { return (int64_t)bt[min(page, page1 - 1)] * Hkv + it.g; };
-    int64_t next0 = tile_of(page_of(0)), next1 = tile_of(page_of(0) + 1);
+    auto id_of = [&](int page) { return bt[min(page, page1 - 1)]; };
+    // (page ids are asked for a step ahead; the opaque copies keep the wait for them where they are used)
+    int32_t next0 = id_of(page_of(0)), next1 = id_of(page_of(0) + 1);
     auto issue = [&](int i) {
-        tr_copy_step<WR, KT, D>(tr_lds_address(ring[i % R][kg]), kc, vc, next0, next1, wr, lane);
-        next0 = tile_of(page_of(i + 1)); next1 = tile_of(page_of(i + 1) + 1);
+        const int64_t tile0 = (int64_t)opaque_uniform(next0) * Hkv + it.g, tile1 = (int64_t)opaque_uniform(next1) * Hkv + it.g;
+        next0 = id_of(page_of(i + 1)); next1 = id_of(page_of(i + 1) + 1);
+        tr_copy_step<WR, KT, D>(tr_lds_address(ring[i % R][kg]), kc, vc, tile0, tile1, wr, lane);
+    };
+    // the copies of a step have landed, those of up to `later` steps behind it may be under way; then everybody's have
+    auto wait = [&](int later) {
+        if (R > 3 && later >= 3) tr_wait_copies<(R > 3 ? 3 * C : 0)>();
+        else if (R > 2 && later == 2) tr_wait_copies<(R > 2 ? 2 * C : 0)>();
+        else if (later == 1) tr_wait_copies<C>();
+        else tr_wait_copies<0>();
+        if constexpr (WR > 1) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     };
 #pragma unroll
-    for (int i = 0; i < R - 1; ++i)
+    for (int i = 0; i < R; ++i)
         if (i < n_step) issue(i);
 
     // scores are wanted in log2 units: s * c; a negative c (e4m3 scale) is taken into Q, so that the maximum can be taken of s
     // (a scale of zero becomes a very small one: what is masked, -inf, keeps a weight of zero)
     const float c_signed = a.sm_scale * (sizeof(KT) == 1 ? a.k_scale[it.g] : 1.0f) * kLog2e;
     const float c = c_signed == 0.0f ? 1e-37f : __builtin_fabsf(c_signed);
-    TrQ<KT, D> q[NT];
-    int node[NT];
+    const int row = first_row + n, row_in = min(row, it.node_rows - 1), node = row_in / G;
+    TrQ<KT, D> q;
+    tr_load_q(q, a.q, ((int64_t)(it.row0 + node) * Hq + it.g * G + row_in % G) * D, h, c_signed < 0.0f);
+    f32x16 acc[DB];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int row = min(first_row + 32 * t + n, it.node_rows - 1);
-        node[t] = row / G;
-        tr_load_q(q[t], a.q, ((int64_t)(it.row0 + node[t]) * Hq + it.g * G + row % G) * D, h, c_signed < 0.0f);
-    }
-    f32x16 acc[NT][DB];
-    float m[NT], l[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        m[t] = kNoKeyTr; l[t] = 0.0f;
-#pragma unroll
-        for (int b = 0; b < DB; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[t][b][i] = 0.0f;
-    }
+    for (int b = 0; b < DB; ++b) acc[b] = f32x16{};
+    float m = kNoKeyTr, l = 0.0f;
 
-    auto step = [&](const unsigned char* lk, int page, auto masked) {
+    TrK<KT, D> k;
+    wait(min(R - 1, n_step - 1));
+    if (works) tr_load_k(k, ring[0][kg], lane);
+    // step i is done with its LDS slot: the next one's K, and copies of step i + R into the slot
+    auto advance = [&](int i) {
+        if (i + 1 >= n_step) return;
+        wait(min(R - 2, n_step - 2 - i));
+        if (i + R < n_step) issue(i + R);
+        if (works) tr_load_k(k, ring[(i + 1) % R][kg], lane);
+    };
+
+    auto step = [&](int i, auto masked) {
         constexpr bool MASKED = decltype(masked)::value;
+        const unsigned char* lk = ring[i % R][kg];
         const unsigned char* lv = lk + S::NK * 1024;
-        f32x16 x[NT];
-        tr_scores<NT, KT, D>(x, lk, q, lane);
-        [[maybe_unused]] uint32_t seen[NT];                    // bits 0 .. 7: tokens 8h .. of the first page, 8 .. 15: of the second
+        const int page = page_of(i);
+        f32x16 x = tr_scores(k, lk, q, lane);
+        // (16-bit arithmetic: V is read while the scores are being made and turned into weights)
+        TrV<KT, D> v[F32 ? 1 : 2][F32 ? 1 : DB];
+        if constexpr (!F32) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int b = 0; b < DB; ++b) v[u][b] = tr_load_v<KT, D>(lv, u, b, lane);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        [[maybe_unused]] uint32_t seen = 0;                    // bits 0 .. 7: tokens 8h .. of the first page, 8 .. 15: of the second
         if constexpr (MASKED) {
+            const int j0 = page * kPage + 8 * h - it.prefix;
+            seen = tr_seen(a, it.row0, it.n_nodes, node, j0) | tr_seen(a, it.row0, it.n_nodes, node, j0 + kPage) << 8;
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const int j0 = page * kPage + 8 * h - it.prefix;
-                seen[t] = tr_seen(a, it.row0, it.n_nodes, node[t], j0) | tr_seen(a, it.row0, it.n_nodes, node[t], j0 + kPage) << 8;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[t][i] = seen[t] >> i & 1 ? x[t][i] : -INFINITY;
-            }
+            for (int e = 0; e < 16; ++e) x[e] = seen >> e & 1 ? x[e] : -INFINITY;
         }
-        float top[NT];
-        bool higher = false;
+        float p[16], sum;
+        auto weigh = [&] {
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            float u[8];
+            for (int e = 0; e < 16; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], c, -m));
+            float t[4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) u[i] = fmaxf(x[t][i], x[t][i + 8]);
-            top[t] = fmaxf(fmaxf(fmaxf(u[0], u[1]), fmaxf(u[2], u[3])), fmaxf(fmaxf(u[4], u[5]), fmaxf(u[6], u[7]))) * c;
-            higher |= top[t] > m[t] + kRaiseTr;
+            for (int e = 0; e < 4; ++e) t[e] = (p[e] + p[e + 4]) + (p[e + 8] + p[e + 12]);
+            sum = (t[0] + t[1]) + (t[2] + t[3]);
+        };
+        weigh();
+        if (__any(sum > kBigTr)) {                             // rare: the reference is raised to the column's maximum
+            float top = x[0];
+#pragma unroll
+            for (int e = 1; e < 16; ++e) top = fmaxf(top, x[e]);
+            const float m_new = fmaxf(m, pair32_max(top) * c);
+            const float alpha = __builtin_amdgcn_exp2f(m - m_new);
+#pragma unroll
+            for (int b = 0; b < DB; ++b) acc[b] *= alpha;
+            l *= alpha;
+            m = m_new;
+            weigh();
         }
-        if (__any(higher)) {                                   // rare
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const float m_new = fmaxf(m[t], pair32_max(top[t]));
-                const float alpha = __builtin_amdgcn_exp2f(m[t] - m_new);
-#pragma unroll
-                for (int b = 0; b < DB; ++b) acc[t][b] *= alpha;
-                l[t] *= alpha;
-                m[t] = m_new;
-            }
-        }
-        float p[NT][16];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                p[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][i], c, -m[t]));
-            }
-            float sum[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sum[i] = (p[t][i] + p[t][i + 4]) + (p[t][i + 8] + p[t][i + 12]);
-            l[t] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        }
+        l += sum;
         [[maybe_unused]] bool odd = false;
+        // (masked) what does not exist does not enter the sums, and what is not finite enters below, in those rows that see it
+        if constexpr (MASKED && !F32) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            [[maybe_unused]] bf16x8 pb[NT];
-            if constexpr (sizeof(KT) != 4) {
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
-                    pb[t] = __builtin_bit_cast(bf16x8, make_uint4(pack_bf16(p[t][8 * u], p[t][8 * u + 1]), pack_bf16(p[t][8 * u + 2], p[t][8 * u + 3]),
-                                                                  pack_bf16(p[t][8 * u + 4], p[t][8 * u + 5]), pack_bf16(p[t][8 * u + 6], p[t][8 * u + 7])));
-            }
+                for (int b = 0; b < DB; ++b) odd |= tr_clean_v(v[u][b], ctx_len - (page + u) * kPage - 8 * h);
+        }
+        bool late = false;                                     // whether the slot is still needed
+        if constexpr (MASKED && !F32) late = __any(odd);
+        if constexpr (!F32) {
+            if (!MASKED) advance(i);
 #pragma unroll
-            for (int b = 0; b < DB; ++b) {
-                TrV<KT, D> v = tr_load_v<KT, D>(lv, u, b, lane);
-                // (masked) what does not exist does not enter the sums, and what is not finite enters below, in those rows that see it
-                if constexpr (MASKED) odd |= tr_clean_v(v, ctx_len - (page + u) * kPage - 8 * h);
-                if constexpr (sizeof(KT) == 4) {
+            for (int u = 0; u < 2; ++u) {
+                const bf16x8 pb = __builtin_bit_cast(bf16x8, make_uint4(pack_bf16(p[8 * u], p[8 * u + 1]), pack_bf16(p[8 * u + 2], p[8 * u + 3]),
+                                                                        pack_bf16(p[8 * u + 4], p[8 * u + 5]), pack_bf16(p[8 * u + 6], p[8 * u + 7])));
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-#pragma unroll
-                        for (int t = 0; t < NT; ++t)
-                            acc[t][b] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(v.w[e]), p[t][8 * u + e], acc[t][b], 0, 0, 0);
-                } else {
+                for (int b = 0; b < DB; ++b) {
                     uint4 w;
-                    if constexpr (sizeof(KT) == 2) w = make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
+                    if constexpr (sizeof(KT) == 2) w = make_uint4(v[u][b].w[0], v[u][b].w[1], v[u][b].w[2], v[u][b].w[3]);
                     else {
-                        const uint2 w0 = tr_widen(v.w[0]), w1 = tr_widen(v.w[1]);
+                        const uint2 w0 = tr_widen(v[u][b].w[0]), w1 = tr_widen(v[u][b].w[1]);
                         w = make_uint4(w0.x, w0.y, w1.x, w1.y);
                     }
-#pragma unroll
-                    for (int t = 0; t < NT; ++t)
-                        acc[t][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), pb[t], acc[t][b], 0, 0, 0);
+                    acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), pb, acc[b], 0, 0, 0);
                 }
             }
+        } else {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int b = 0; b < DB; ++b) {
+                    TrV<KT, D> w = tr_load_v<KT, D>(lv, u, b, lane);
+                    if constexpr (MASKED) odd |= tr_clean_v(w, ctx_len - (page + u) * kPage - 8 * h);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) acc[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(w.w[e]), p[8 * u + e], acc[b], 0, 0, 0);
+                }
+            if constexpr (MASKED) late = __any(odd);
         }
         if constexpr (MASKED) {
-            if (__any(odd)) {
+            if (late) {
                 // How many values of +inf (or NaN) and of -inf (or NaN) a row sees of a dim: products of zeros and ones.
                 for (int u = 0; u < 2; ++u) {                  // (not unrolled: rarely taken)
                     const int have = ctx_len - (page + u) * kPage - 8 * h;
-                    uint4 on[NT];
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        const uint32_t bits = seen[t] >> (8 * u);
-                        auto two = [&](int e) { return (bits >> e & 1 ? 0x3f80u : 0u) | (bits >> (e + 1) & 1 ? 0x3f800000u : 0u); };
-                        on[t] = make_uint4(two(0), two(2), two(4), two(6));
-                    }
+                    const uint32_t bits = seen >> (8 * u);
+                    auto two = [&](int e) { return (bits >> e & 1 ? 0x3f80u : 0u) | (bits >> (e + 1) & 1 ? 0x3f800000u : 0u); };
+                    const bf16x8 on = __builtin_bit_cast(bf16x8, make_uint4(two(0), two(2), two(4), two(6)));
 #pragma unroll
                     for (int b = 0; b < DB; ++b) {
-                        const TrV<KT, D> v = tr_load_v<KT, D>(lv, u, b, lane);
+                        const TrV<KT, D> w = tr_load_v<KT, D>(lv, u, b, lane);
                         uint32_t plus[4] = {}, minus[4] = {};
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
-                            const float f = tr_element(v, e);
+                            const float f = tr_element(w, e);
                             plus[e / 2] |= e < have && !(f < INFINITY) ? 0x3f80u << (16 * (e & 1)) : 0u;
                             minus[e / 2] |= e < have && !(f > -INFINITY) ? 0x3f80u << (16 * (e & 1)) : 0u;
                         }
+                        const f32x16 zero = {};
+                        const f32x16 np = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, make_uint4(plus[0], plus[1], plus[2], plus[3])), on, zero, 0, 0, 0);
+                        const f32x16 nm = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, make_uint4(minus[0], minus[1], minus[2], minus[3])), on, zero, 0, 0, 0);
 #pragma unroll
-                        for (int t = 0; t < NT; ++t) {
-                            f32x16 zero = {};
-                            const f32x16 np = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, make_uint4(plus[0], plus[1], plus[2], plus[3])), __builtin_bit_cast(bf16x8, on[t]), zero, 0, 0, 0);
-                            const f32x16 nm = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, make_uint4(minus[0], minus[1], minus[2], minus[3])), __builtin_bit_cast(bf16x8, on[t]), zero, 0, 0, 0);
-#pragma unroll
-                            for (int r = 0; r < 16; ++r) {
-                                if (np[r] > 0.0f) acc[t][b][r] += INFINITY;
-                                if (nm[r] > 0.0f) acc[t][b][r] -= INFINITY;
-                            }
+                        for (int r = 0; r < 16; ++r) {
+                            if (np[r] > 0.0f) acc[b][r] += INFINITY;
+                            if (nm[r] > 0.0f) acc[b][r] -= INFINITY;
                         }
                     }
                 }
             }
         }
+        if (F32 || MASKED) advance(i);
     };
 
-    const int plain = it.prefix / kPage;                       // pages whose keys everybody sees
-    auto round = [&](int i, auto masked) {
-        // the copies of step i have landed (up to R - 2 later ones may be under way), and everybody is done with step i - 1
-        const int later = min(R - 2, n_step - 1 - i);
-        if (R > 3 && later == 2) tr_wait_copies<(R > 3 ? 2 * C : 0)>();
-        else if (R > 2 && later == 1) tr_wait_copies<(R > 2 ? C : 0)>();
-        else tr_wait_copies<0>();
-        if constexpr (WR > 1) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (i + R - 1 < n_step) issue(i + R - 1);
-        if (works) step(ring[i % R][kg], page_of(i), masked);
-    };
+    // pages whose keys everybody sees, then those that hold nodes
+    const int plain = min(it.prefix / kPage, page1);
+    auto one = [&](int i, auto masked) { if (works) step(i, masked); else advance(i); };
     int i = 0;
-    for (; page0 + 2 * WK * (i + 1) <= min(plain, page1); ++i) round(i, std::false_type{});
-    for (; i < n_step; ++i) round(i, std::true_type{});
+    for (; page0 + 2 * WK * (i + 1) <= plain; ++i) one(i, std::false_type{});
+    for (; i < n_step; ++i) one(i, std::true_type{});
 
     // the waves of other keys hand over their states through LDS: every lane's registers as they are
-#pragma unroll
-    for (int t = 0; t < NT; ++t) l[t] = pair32_sum(l[t]);      // (both lanes of a column hold the same reference)
+    l = pair32_sum(l);                                         // (both lanes of a column hold the same reference)
     if constexpr (WK > 1) {
         float* state = (float*)&ring[0][0][0];
-        constexpr int kState = NT * DB * 1024 + NT * 64;       // words of a wave
+        constexpr int kState = DB * 1024 + 64;                 // words of a wave
         float* mine = state + (wave - WR) * kState;
         __syncthreads();                                       // (nobody reads or fills the ring any more)
         if (kg > 0) {
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
+            for (int b = 0; b < DB; ++b)
 #pragma unroll
-                for (int b = 0; b < DB; ++b)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        *(f32x4*)(mine + ((t * DB + b) * 4 + r) * 256 + lane * 4) = f32x4{acc[t][b][4 * r], acc[t][b][4 * r + 1], acc[t][b][4 * r + 2], acc[t][b][4 * r + 3]};
-                if (h == 0) *(f32x2*)(mine + NT * DB * 1024 + t * 64 + 2 * n) = f32x2{m[t], l[t]};
-            }
+                for (int r = 0; r < 4; ++r)
+                    *(f32x4*)(mine + (b * 4 + r) * 256 + lane * 4) = f32x4{acc[b][4 * r], acc[b][4 * r + 1], acc[b][4 * r + 2], acc[b][4 * r + 3]};
+            if (h == 0) *(f32x2*)(mine + DB * 1024 + 2 * n) = f32x2{m, l};
         }
         __syncthreads();
         if (kg > 0) return;
+        auto ml_of = [&](int k) { return *(const f32x2*)(state + (k * WR + wr - WR) * kState + DB * 1024 + 2 * n); };
+        float top = m;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            auto ml_of = [&](int k) { return *(const f32x2*)(state + (k * WR + wr - WR) * kState + NT * DB * 1024 + t * 64 + 2 * n); };
-            float top = m[t];
+        for (int w = 1; w < WK; ++w) top = fmaxf(top, ml_of(w).x);
+        const float f0 = __builtin_amdgcn_exp2f(m - top);
+        l *= f0;
 #pragma unroll
-            for (int k = 1; k < WK; ++k) top = fmaxf(top, ml_of(k).x);
-            const float f0 = __builtin_amdgcn_exp2f(m[t] - top);
-            l[t] *= f0;
-#pragma unroll
-            for (int b = 0; b < DB; ++b) acc[t][b] *= f0;
+        for (int b = 0; b < DB; ++b) acc[b] *= f0;
 #pragma unroll 1
-            for (int k = 1; k < WK; ++k) {                     // (in the order of the waves)
-                const f32x2 ml = ml_of(k);
-                const float f = __builtin_amdgcn_exp2f(ml.x - top);
-                const float* other = state + (k * WR + wr - WR) * kState;
-                l[t] += ml.y * f;
+        for (int w = 1; w < WK; ++w) {                         // (in the order of the waves)
+            const f32x2 ml = ml_of(w);
+            const float f = __builtin_amdgcn_exp2f(ml.x - top);
+            const float* other = state + (w * WR + wr - WR) * kState;
+            l += ml.y * f;
 #pragma unroll
-                for (int b = 0; b < DB; ++b)
+            for (int b = 0; b < DB; ++b)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const f32x4 o = *(const f32x4*)(other + ((t * DB + b) * 4 + r) * 256 + lane * 4);
+                for (int r = 0; r < 4; ++r) {
+                    const f32x4 o = *(const f32x4*)(other + (b * 4 + r) * 256 + lane * 4);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) acc[t][b][4 * r + j] += o[j] * f;
-                    }
-            }
-            m[t] = top;
+                    for (int j = 0; j < 4; ++j) acc[b][4 * r + j] += o[j] * f;
+                }
         }
+        m = top;
     }
-    if (!works) return;
-    const float vscale = sizeof(KT) == 1 ? a.v_scale[it.g] : 1.0f;
+    if (!works || row >= it.node_rows) return;
+    if (it.parts == 1) {
+        const float inv = tr_inverse(a, l, it.prefix, it.n_nodes, it.row0, node) * (sizeof(KT) == 1 ? a.v_scale[it.g] : 1.0f);
+        const int64_t at = ((int64_t)(it.row0 + node) * Hq + it.g * G + row % G) * D + 4 * h;
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int row = first_row + 32 * t + n;
-        if (row >= it.node_rows) continue;
-        if (it.parts == 1) {
-            const float inv = tr_inverse(a, l[t], it.prefix, it.n_nodes, it.row0, node[t]) * vscale;
-            const int64_t at = ((int64_t)(it.row0 + node[t]) * Hq + it.g * G + row % G) * D + 4 * h;
+        for (int b = 0; b < DB; ++b)
 #pragma unroll
-            for (int b = 0; b < DB; ++b)
+            for (int r = 0; r < 4; ++r)
+                tr_store_out<KT>(a, at + 32 * b + 8 * r, f32x4{acc[b][4 * r], acc[b][4 * r + 1], acc[b][4 * r + 2], acc[b][4 * r + 3]} * inv);
+    } else {
+        const int64_t at = it.part_row0 + ((int64_t)it.g * it.parts + it.part) * it.node_rows + row;
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    tr_store_out<KT>(a, at + 32 * b + 8 * r, f32x4{acc[t][b][4 * r], acc[t][b][4 * r + 1], acc[t][b][4 * r + 2], acc[t][b][4 * r + 3]} * inv);
-        } else {
-            const int64_t at = it.part_row0 + ((int64_t)it.g * it.parts + it.part) * it.node_rows + row;
+        for (int b = 0; b < DB; ++b)
 #pragma unroll
-            for (int b = 0; b < DB; ++b)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    *(f32x4*)(a.part_o + at * D + 4 * h + 32 * b + 8 * r) = f32x4{acc[t][b][4 * r], acc[t][b][4 * r + 1], acc[t][b][4 * r + 2], acc[t][b][4 * r + 3]};
-            if (h == 0) *(f32x2*)(a.part_ml + 2 * at) = f32x2{m[t], l[t]};
-        }
+            for (int r = 0; r < 4; ++r)
+                *(f32x4*)(a.part_o + at * D + 4 * h + 32 * b + 8 * r) = f32x4{acc[b][4 * r], acc[b][4 * r + 1], acc[b][4 * r + 2], acc[b][4 * r + 3]};
+        if (h == 0) *(f32x2*)(a.part_ml + 2 * at) = f32x2{m, l};
     }
 }
 
-// Rows whose scan was cut: D / 4 threads per row add up its parts in order.
+// Rows whose scan was cut: a wave per row, four dims per lane: with 128 dims the two halves of the wave
+// take every other part, with 64 dims the four quarters every fourth.  Eight parts of each are read together.
 template <typename KT, int D>
 __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, TreeSeqs s, int n_rows)
 {
-    constexpr int TPR = D / 4;
-    const int w = blockIdx.x * (256 / TPR) + threadIdx.x / TPR, d4 = threadIdx.x % TPR;
-    // (the rows of a workgroup may belong to several sequences: every lane looks for its own)
-    int i = 0;
-    for (int b = 1; b < s.n; ++b) i += s.seq[b].first_merge <= w ? 1 : 0;
+    constexpr int SHARES = 256 / D;                            // parts side by side in a wave
+    const int lane = threadIdx.x & 63, share = lane / (D / 4), d4 = lane % (D / 4);
+    const int w = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
     if (w >= n_rows) return;
-    const TreeSeq q = s.seq[i];
-    const int n_nodes = s.seq[i + 1].row0 - q.row0, rows = n_nodes * a.geo.G, k = w - q.first_merge, g = k / rows, row = k % rows;
+    int i = -1;
+#pragma unroll
+    for (int b = 0; b < kTreeSeqs; b += 64) {
+        const int k = min(b + lane, kTreeSeqs - 1);
+        i += __builtin_popcountll(__ballot((b + lane < s.n) & (s.seq[k].first_merge <= w)));
+    }
+    // (sequences that were not cut share the number of the next one that was: the last match counts, unless it is one behind the last cut one)
+    TreeSeq q = s.seq[i];
+    while (q.parts < 2) q = s.seq[--i];
+    const int rows = q.n_nodes * a.geo.G, k = w - q.first_merge, g = k / rows, row = k % rows;
     const int64_t at = q.part_row0 + (int64_t)g * q.parts * rows + row;
-    // (eight parts at a time: their loads wait together)
     float top = kNoKeyTr, sum = 0.0f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int p0 = 0; p0 < q.parts; p0 += 8) {
+    for (int p0 = share; p0 - share < q.parts; p0 += 8 * SHARES) {
         f32x2 ml[8];
         f32x4 v[8];
 #pragma unroll
-        for (int p = 0; p < 8; ++p) ml[p] = *(const f32x2*)(a.part_ml + 2 * (at + (int64_t)min(p0 + p, q.parts - 1) * rows));
-#pragma unroll
-        for (int p = 0; p < 8; ++p) v[p] = *(const f32x4*)(a.part_o + (at + (int64_t)min(p0 + p, q.parts - 1) * rows) * D + 4 * d4);
+        for (int j = 0; j < 8; ++j) {
+            ml[j] = f32x2{kNoKeyTr, 0.0f};
+            v[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (p0 - share + j * SHARES < q.parts) {           // (the same for the wave)
+                const int64_t from = at + (int64_t)min(p0 + j * SHARES, q.parts - 1) * rows;
+                ml[j] = *(const f32x2*)(a.part_ml + 2 * from);
+                v[j] = *(const f32x4*)(a.part_o + from * D + 4 * d4);
+            }
+        }
         float m = top;
 #pragma unroll
-        for (int p = 0; p < 8; ++p) m = fmaxf(m, ml[p].x);
+        for (int j = 0; j < 8; ++j) m = fmaxf(m, ml[j].x);     // (a part that is read twice changes nothing here)
         const float f0 = __builtin_amdgcn_exp2f(top - m);
         o *= f0; sum *= f0; top = m;
 #pragma unroll
-        for (int p = 0; p < 8; ++p) {
-            if (p0 + p >= q.parts) continue;
-            const float f = __builtin_amdgcn_exp2f(ml[p].x - top);
-            o += v[p] * f;
-            sum += ml[p].y * f;
+        for (int j = 0; j < 8; ++j) {
+            const bool in = p0 + j * SHARES < q.parts;
+            const float f = __builtin_amdgcn_exp2f(ml[j].x - top);
+            const f32x4 add = v[j] * f;
+            o = in ? o + add : o;
+            sum = in ? sum + ml[j].y * f : sum;
         }
     }
+    // the shares meet: quarters first, then halves
+    auto meet = [&](int step) {
+        const float m = fmaxf(top, __shfl_xor(top, step, 64));
+        const float f = __builtin_amdgcn_exp2f(top - m);
+        o *= f; sum *= f; top = m;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] += __shfl_xor(o[j], step, 64);
+        sum += __shfl_xor(sum, step, 64);
+    };
+    if constexpr (SHARES == 4) meet(16);
+    meet(32);
     const int nd = row / a.geo.G;
-    const float inv = tr_inverse(a, sum, q.prefix, n_nodes, q.row0, nd) * (sizeof(KT) == 1 ? a.v_scale[g] : 1.0f);
-    tr_store_out<KT>(a, ((int64_t)(q.row0 + nd) * a.geo.Hq + g * a.geo.G + row % a.geo.G) * D + 4 * d4, o * inv);
+    const float inv = tr_inverse(a, sum, q.prefix, q.n_nodes, q.row0, nd) * (sizeof(KT) == 1 ? a.v_scale[g] : 1.0f);
+    if (share == 0) tr_store_out<KT>(a, ((int64_t)(q.row0 + nd) * a.geo.Hq + g * a.geo.G + row % a.geo.G) * D + 4 * d4, o * inv);
 }
 
 template <typename KT, int D>
 static int launch_tree_d(const TreeArgs& a, const TreeSeqs& s, int64_t items, hipStream_t st, hipEvent_t done)
 {
     const dim3 grid((unsigned)items), block(64 * kTrWaves);
-    if (a.rows == 64) return launch_kernel(tree_kernel<KT, D, 2, 1>, grid, block, st, done, a, s);
-    if (a.rows == 128) return launch_kernel(tree_kernel<KT, D, 4, 1>, grid, block, st, done, a, s);
+    if (a.rows == 64) return launch_kernel(tree_kernel<KT, D, 2>, grid, block, st, done, a, s);
+    if (a.rows == 128) return launch_kernel(tree_kernel<KT, D, 4>, grid, block, st, done, a, s);
     if constexpr (sizeof(KT) != 4) {
-        if (a.rows == 32) return launch_kernel(tree_kernel<KT, D, 1, 1>, grid, block, st, done, a, s);
+        if (a.rows == 32) return launch_kernel(tree_kernel<KT, D, 1>, grid, block, st, done, a, s);
     }
     return (int)hipErrorInvalidValue;
 }
@@ -594,8 +609,7 @@ int launch_tree_merge(const TreeArgs& a, const TreeSeqs& s, int32_t rows, void* 
     hipStream_t st = (hipStream_t)stream;
     hipEvent_t ev = (hipEvent_t)done;
     const bool d128 = a.geo.D == 128;
-    const int per = 256 / (a.geo.D / 4);
-    const dim3 grid((unsigned)((rows + per - 1) / per)), block(256);
+    const dim3 grid((unsigned)((rows + 3) / 4)), block(256);
     if (a.geo.q_dtype == TS_F32) return d128 ? launch_kernel(tree_merge_kernel<float, 128>, grid, block, st, ev, a, s, rows) : launch_kernel(tree_merge_kernel<float, 64>, grid, block, st, ev, a, s, rows);
     if (a.geo.kv_dtype == TS_BF16) return d128 ? launch_kernel(tree_merge_kernel<uint16_t, 128>, grid, block, st, ev, a, s, rows) : launch_kernel(tree_merge_kernel<uint16_t, 64>, grid, block, st, ev, a, s, rows);
     return d128 ? launch_kernel(tree_merge_kernel<uint8_t, 128>, grid, block, st, ev, a, s, rows) : launch_kernel(tree_merge_kernel<uint8_t, 64>, grid, block, st, ev, a, s, rows);

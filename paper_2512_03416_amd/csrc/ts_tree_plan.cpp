@@ -1,6 +1,8 @@
 // Host side of the rotary append and of the attention of drafted trees: frequencies, masks, how a batch is cut.
 #include <algorithm>
 #include <cmath>
+#include <functional>
+#include <utility>
 
 #include "ts_internal.h"
 
@@ -72,36 +74,108 @@ int32_t rope_heads_per_slice(const ts_attn_desc& d, int64_t units, int n_cu)
     return heads;
 }
 
-// A scan with less than a round of workgroups is cut along the keys, into pieces of at least kMinPages pages.
-constexpr int32_t kMinPages = 16;
-
-TreePlan plan_tree(const ts_attn_desc& d, const int32_t* q_lens, const int32_t* ctx_lens, int num_seqs, int n_cu)
+// Times of the tree kernel in us, measured, from which the cuts are chosen.  They need to be right to a third or so.
+struct TreeTimes {
+    double page_alone;                 // a page (K and V of one KV head) of a workgroup that has the GPU to itself: bound by latency, in
+                                       // proportion to the waves that share it (64-row workgroups take two pages at a time)
+    double page_full;                  // the same with a workgroup in every place: bound by the matrix products and the softmax
+    double page_read;                  // a page read from HBM, by whichever of its groups of rows comes first
+    int64_t places;                    // workgroups resident at once
+    double start, round;               // launch, page ids, queries, first copies, last stores; of a later workgroup in the same place
+    double merge, merge_row;           // merge launch, and a partial row written and read again
+};
+static TreeTimes tree_times(const ts_attn_desc& d, int rows, int n_cu)
 {
-    TreePlan p;
+    const int elem = d.kv_dtype == TS_F32 ? 4 : (d.kv_dtype == TS_BF16 ? 2 : 1);
+    const int slot = 2 * kTreeWaves * 32 / rows * 2 * kPage * d.head_dim * elem;
+    const double dims = d.head_dim / 128.0, math = d.q_dtype == TS_F32 ? 8.0 : 1.0;
+    TreeTimes t;
+    t.places = (int64_t)n_cu * std::max(1, std::min(2, 160 * 1024 / (slot * tree_ring_slots(slot))));
+    const double per_cu = (double)t.places / n_cu;
+    t.page_alone = 0.36 * rows / 128 * (0.3 + 0.7 * dims) * math;
+    t.page_full = 0.27 * per_cu * rows / 128 * dims * math;    // 0.54 with 128 rows and two workgroups per CU
+    t.page_read = 2.0 * kPage * d.head_dim * elem / 6.2e6;     // 6.2 TB/s
+    t.start = 5.0;
+    t.round = 2.5;
+    t.merge = 6.0;
+    t.merge_row = 8.0 * d.head_dim / 4e6;
+    return t;
+}
+
+// Uncut, a scan writes no partial results, and the longest scans come first, so that a batch with a workgroup or more for every place
+// comes out even by itself: 32 trees of 32-64 nodes over 1-8 Ki tokens (64/8 heads) take 284 us uncut, 297 in ranges of at most 384
+// pages, 317 in ranges of 192.  Smaller batches are cut until the workgroups fill the places: 8 trees of 30 nodes over 4000 tokens
+// (32/8 heads) 92 us uncut, 38 in ranges of 32 to 64 pages, 54 in ranges of 16 (most of it partial results).  Ranges of a sequence are of
+// one length.
+void plan_tree(const ts_attn_desc& d, const int32_t* q_lens, const int32_t* ctx_lens, int num_seqs, int n_cu, TreePlan* plan)
+{
     const int32_t G = d.num_q_heads / d.num_kv_heads, Hkv = d.num_kv_heads;
-    int64_t most = 0;
+    plan->seqs.clear();
+    int64_t most = 0, row = 0, total = 0;
     int32_t longest = 0;
-    for (int s = 0; s < num_seqs; ++s)
-        if (q_lens[s] > 0) { most = std::max<int64_t>(most, (int64_t)q_lens[s] * G); longest = std::max(longest, ctx_lens[s]); }
-    p.rows = most <= 32 && d.q_dtype != TS_F32 ? 32 : (most <= 64 ? 64 : 128);
-    int64_t pages = 0;                                     // pages read, over the workgroups' groups of rows
-    for (int s = 0; s < num_seqs; ++s)
-        if (q_lens[s] > 0) pages += (int64_t)tree_groups(q_lens[s], G, p.rows) * ((ctx_lens[s] + kPage - 1) / kPage) * Hkv;
-    const int64_t slots = (int64_t)n_cu * 2;
-    int64_t part = std::max<int64_t>(kMinPages, (pages + slots - 1) / slots);
-    const int64_t whole = (longest + kPage - 1) / kPage;
-    for (;; part *= 2) {
-        part = std::min<int64_t>((part + 7) / 8 * 8, (whole + 7) / 8 * 8);     // (whole rounds of the waves)
-        p.part_pages = (int32_t)part;
-        p.part_rows = p.items = 0;
-        for (int s = 0; s < num_seqs; ++s) {
-            if (q_lens[s] <= 0) continue;
-            const int64_t n = tree_parts(ctx_lens[s], p.part_pages);
-            p.items += n * Hkv * tree_groups(q_lens[s], G, p.rows);
-            if (n > 1) p.part_rows += n * Hkv * G * q_lens[s];
+    auto pages_of = [](const TreeSeq& s) { return (s.prefix + s.n_nodes + kPage - 1) / kPage; };
+    for (int s = 0; s < num_seqs; ++s) {
+        if (q_lens[s] > 0) {
+            most = std::max<int64_t>(most, (int64_t)q_lens[s] * G);
+            plan->seqs.push_back(TreeSeq{s, (int32_t)row, q_lens[s], ctx_lens[s] - q_lens[s], 0, 1, 0, 0, 0});
+            longest = std::max(longest, pages_of(plan->seqs.back()));
         }
-        if (p.part_rows <= kTreePartRows || part >= whole) return p;
+        row += q_lens[s];
     }
+    plan->rows = most <= 32 && d.q_dtype != TS_F32 ? 32 : (most <= 64 ? 64 : 128);
+    const int32_t round = 2 * kTreeWaves * 32 / plan->rows;    // pages that a workgroup's waves take in turn
+    auto groups_of = [&](const TreeSeq& s) { return tree_groups(s.n_nodes, G, plan->rows); };
+    int64_t scans = 0;                                         // pages of all scans, and of all scans' groups of rows
+    for (const TreeSeq& s : plan->seqs) { scans += pages_of(s); total += (int64_t)pages_of(s) * groups_of(s); }
+    const TreeTimes t = tree_times(d, plan->rows, n_cu);
+    auto cut_to = [&](int32_t L) {                             // ranges of at most L pages (a multiple of round)
+        for (TreeSeq& s : plan->seqs) {
+            const int32_t pages = pages_of(s), parts = (pages + L - 1) / L;
+            s.part_pages = ((pages + parts - 1) / parts + round - 1) / round * round;
+            s.parts = (pages + s.part_pages - 1) / s.part_pages;
+        }
+    };
+    const int32_t whole = (longest + round - 1) / round * round;
+    std::vector<std::pair<int32_t, int32_t>> ranges;
+    int32_t best = whole;
+    double best_time = 0.0;
+    for (int32_t L = whole; L >= round; L = std::min((L / 4 * 3 + round - 1) / round * round, L - round)) {
+        int64_t items = 0, rows = 0;
+        int32_t len = 0;
+        cut_to(L);
+        for (const TreeSeq& s : plan->seqs) {
+            items += (int64_t)s.parts * Hkv * groups_of(s);
+            len = std::max(len, std::min(s.part_pages, pages_of(s)));
+            if (s.parts > 1) rows += (int64_t)s.parts * s.n_nodes * d.num_q_heads;
+        }
+        if (rows > kTreePartRows) break;                       // (shorter ranges have more of them)
+        const double fill = std::min(1.0, (double)items / t.places), page = std::max(t.page_alone, t.page_full * fill);
+        // the longest range, or all of them on the places they have (one behind the other, the shortest last, leaves a little
+        // unevenness), or HBM
+        double time = std::max(len * t.page_alone, (double)total * Hkv / std::min<int64_t>(items, t.places) * page);
+        if (items > n_cu && items <= t.places) {               // the longest ranges share their CUs with those from number n_cu on
+            ranges.clear();
+            for (const TreeSeq& s : plan->seqs) ranges.push_back({std::min(s.part_pages, pages_of(s)), s.parts * Hkv * groups_of(s)});
+            std::sort(ranges.begin(), ranges.end(), std::greater<>());
+            int64_t before = 0;
+            size_t k = 0;
+            while (k + 1 < ranges.size() && before + ranges[k].second <= n_cu) before += ranges[k++].second;
+            time = std::max(time, 0.85 * (len * t.page_alone + ranges[k].first * std::max(0.0, t.page_full - t.page_alone)));
+        }
+        if (items > t.places) time += 0.15 * page * total * Hkv / items + ((double)items / t.places - 1.0) * t.round;
+        time = t.start + std::max(time, scans * Hkv * t.page_read);
+        if (rows > 0) time += t.merge + rows * t.merge_row;
+        if (L == whole || time < best_time) { best = L; best_time = time; }
+        if (items > 4 * t.places) break;
+    }
+    cut_to(best);
+    plan->part_rows = 0;
+    for (TreeSeq& s : plan->seqs)
+        if (s.parts > 1) {
+            s.part_row0 = (int32_t)plan->part_rows;
+            plan->part_rows += (int64_t)s.parts * s.n_nodes * d.num_q_heads;
+        }
+    std::stable_sort(plan->seqs.begin(), plan->seqs.end(), [&](const TreeSeq& x, const TreeSeq& y) { return std::min(x.part_pages, pages_of(x)) > std::min(y.part_pages, pages_of(y)); });
 }
 
 }  // namespace ts
