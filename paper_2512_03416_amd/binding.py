@@ -191,25 +191,22 @@ def _dev_ptr(t) -> int:
     return t.data_ptr()
 
 
-def _rows_ptr(t, heads: int, dim: int):
-    """(device pointer, elements from row to row) of token rows [T, heads, dim], whose heads and dims are packed."""
-    if t is None:
-        return 0, 0
-    if not t.is_cuda:
-        raise ValueError("expected a GPU tensor")
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
-        raise ValueError(f"rows of shape {tuple(t.shape)}, expected [tokens, {heads}, {dim}]")
-    if t.shape[0] == 0:
-        return 0, 0
-    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
-        raise ValueError("a row's heads and dims must be packed")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else 0
-
-
 def _i32_bytes(a) -> bytes:
     """int32 values as bytes, which a void* argument takes as they are (host arrays are consumed by the call).
     A quarter of the time of going through numpy's ctypes interface, twice per pass."""
     return np.asarray(a, dtype=np.int32).tobytes()
+
+
+def _host_lens(first, *others):
+    """([int32 arrays as bytes], their common length, the sum of the first one)."""
+    arrays = [np.asarray(a, dtype=np.int32) for a in (first, *others)]
+    n = arrays[0].size
+    for a in arrays:
+        if a.size != n:
+            raise ValueError(f"lengths of {[x.size for x in arrays]} sequences")
+    # (adding up a short list takes a tenth of numpy's sum)
+    total = sum(arrays[0].reshape(-1).tolist()) if n < 64 else int(arrays[0].sum(dtype=np.int64))
+    return [a.tobytes() for a in arrays], n, total
 
 
 def _count(lens) -> int:
@@ -310,7 +307,10 @@ class Context:
         self.desc = desc
         self.device = device
         self._cache_bytes = cache_bytes(desc)
-        self._q_type = ("float32",) if desc.q_dtype == DTYPES["f32"] else ("bfloat16",)
+        self._hq, self._hkv, self._dim, self._width = desc.num_q_heads, desc.num_kv_heads, desc.head_dim, desc.max_pages_per_seq
+        import torch
+        self._f32, self._i32, self._i64 = torch.float32, torch.int32, torch.int64
+        self._q_type = torch.float32 if desc.q_dtype == DTYPES["f32"] else torch.bfloat16
         self._h = ctypes.c_void_p(0)
         rc = self._lib.ts_create(ctypes.byref(desc), device, ctypes.byref(self._h))
         if rc != TS_OK:
@@ -380,50 +380,68 @@ class Context:
         desc = RopeDesc.make(rot_dim, **kw)
         self._check(self._lib.ts_set_rope(self._h, ctypes.byref(desc)))
 
-    @staticmethod
-    def _lens(first, *others):
-        """HOST int32 arrays of one length."""
-        got = [_i32(a).reshape(-1) for a in (first, *others)]
-        if any(a.size != got[0].size for a in got):
-            raise ValueError(f"lengths of {[a.size for a in got]} sequences")
-        return got
+    # The following calls check their tensors: a wrong size or device would not be noticed before the GPU reads past an end.  (Written
+    # for few Python operations: a call of a few short sequences takes the GPU about 5 us.)
 
-    def _tensors(self, **named):
-        """Element types, sizes and device of tensors that are not only handed through: name = (tensor, element type, elements
-        or None)."""
-        for name, (t, dtype, n) in named.items():
-            if t is None or isinstance(t, int):
-                continue
-            if not t.is_cuda or t.device.index != self.device:
-                raise ValueError(f"{name} is on {t.device}, the context on GPU {self.device}")
-            if dtype and str(t.dtype).replace("torch.", "") not in dtype:
-                raise ValueError(f"{name} is {t.dtype}, expected {' or '.join(dtype)}")
-            if n is not None and t.numel() < n:
-                raise ValueError(f"{name} has {t.numel()} elements, needs {n}")
+    def _ptr(self, t, name: str, dtype, n: int) -> int:
+        """Device pointer of a packed tensor of at least n elements of dtype (None = any) on this context's GPU."""
+        if t is None:
+            return 0
+        if t.__class__ is int:
+            return t
+        if t.get_device() != self.device:
+            raise ValueError(f"{name} is on {t.device}, the context on GPU {self.device}")
+        if dtype is not None and t.dtype is not dtype:
+            raise ValueError(f"{name} is {t.dtype}, expected {dtype}")
+        if t.numel() < n:
+            raise ValueError(f"{name} has {t.numel()} elements, needs {n}")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+        return t.data_ptr()
 
-    def _common(self, k_cache, v_cache, k_scale, v_scale, block_table, num_seqs):
-        need = self._cache_bytes
-        for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
-            if t is not None and not isinstance(t, int) and t.numel() * t.element_size() < need:
-                raise ValueError(f"{name} has {t.numel() * t.element_size()} bytes, needs {need}")
-        heads = self.desc.num_kv_heads
-        self._tensors(k_cache=(k_cache, None, None), v_cache=(v_cache, None, None), k_scale=(k_scale, ("float32",), heads),
-                      v_scale=(v_scale, ("float32",), heads),
-                      block_table=(block_table, ("int32",), num_seqs * self.desc.max_pages_per_seq))
+    def _rows(self, t, name: str, heads: int, total: int):
+        """(device pointer, elements from row to row) of token rows [tokens, heads, dim], whose heads and dims are packed."""
+        if t is None:
+            return 0, 0
+        dim, shape = self._dim, t.shape
+        if len(shape) != 3 or shape[1] != heads or shape[2] != dim or shape[0] < total:
+            raise ValueError(f"{name} has shape {tuple(shape)}, expected [{total}, {heads}, {dim}]")
+        if total == 0:
+            return 0, 0
+        if t.get_device() != self.device:
+            raise ValueError(f"{name} is on {t.device}, the context on GPU {self.device}")
+        if t.dtype is not self._q_type:
+            raise ValueError(f"{name} is {t.dtype}, expected {self._q_type}")
+        row, head, one = t.stride()
+        if one != 1 or (head != dim and heads > 1):
+            raise ValueError(f"{name}: a row's heads and dims must be packed")
+        return t.data_ptr(), row if total > 1 else 0
+
+    def _cache_ptr(self, t, name: str) -> int:
+        if t is None:
+            return 0
+        if t.__class__ is int:
+            return t
+        n = t.numel()
+        if n < self._cache_bytes and n * t.element_size() < self._cache_bytes:
+            raise ValueError(f"{name} has {n * t.element_size()} bytes, needs {self._cache_bytes}")
+        if t.get_device() != self.device:
+            raise ValueError(f"{name} is on {t.device}, the context on GPU {self.device}")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+        return t.data_ptr()
 
     def rope_kv_append(self, q, k_new, v_new, q_out, k_cache, v_cache, k_scale, v_scale, block_table, q_lens, ctx_lens,
                        positions=None, stream=None):
         """q, k_new, v_new: [T, heads, dim], rows may be strided (slices of one projection's output); q_out packed, may be q."""
-        d, (ql, cl) = self.desc, self._lens(q_lens, ctx_lens)
-        total, el = int(ql.sum()), self._q_type
-        self._common(k_cache, v_cache, k_scale, v_scale, block_table, ql.size)
-        self._tensors(q=(q, el, total * d.num_q_heads * d.head_dim), k_new=(k_new, el, total * d.num_kv_heads * d.head_dim),
-                      v_new=(v_new, el, total * d.num_kv_heads * d.head_dim), q_out=(q_out, el, total * d.num_q_heads * d.head_dim),
-                      positions=(positions, ("int32",), total))
-        q_rows, k_rows, v_rows = (_rows_ptr(t, h, d.head_dim) for t, h in ((q, d.num_q_heads), (k_new, d.num_kv_heads), (v_new, d.num_kv_heads)))
-        rc = self._lib.ts_rope_kv_append(self._h, self._stream(stream), *q_rows, *k_rows, *v_rows, _dev_ptr(q_out), _dev_ptr(k_cache),
-                                         _dev_ptr(v_cache), _dev_ptr(k_scale), _dev_ptr(v_scale), _dev_ptr(block_table),
-                                         _dev_ptr(positions), ql.tobytes(), cl.tobytes(), ql.size)
+        ptr, rows, hq, hkv = self._ptr, self._rows, self._hq, self._hkv
+        (ql, cl), n, total = _host_lens(q_lens, ctx_lens)
+        rc = self._lib.ts_rope_kv_append(self._h, self._stream(stream), *rows(q, "q", hq, total), *rows(k_new, "k_new", hkv, total),
+                                         *rows(v_new, "v_new", hkv, total), ptr(q_out, "q_out", self._q_type, total * hq * self._dim),
+                                         self._cache_ptr(k_cache, "k_cache"), self._cache_ptr(v_cache, "v_cache"),
+                                         ptr(k_scale, "k_scale", self._f32, hkv), ptr(v_scale, "v_scale", self._f32, hkv),
+                                         ptr(block_table, "block_table", self._i32, n * self._width),
+                                         ptr(positions, "positions", self._i32, total), ql, cl, n)
         if rc != TS_OK:
             self._check(rc)
 
@@ -434,41 +452,46 @@ class Context:
     def tree_attention(self, q, k_cache, v_cache, k_scale, v_scale, block_table, tree_mask, q_lens, ctx_lens, sm_scale: float, out,
                        stream=None):
         """tree_mask: int64 [T, words] on the GPU (see tree_masks), or None for chains."""
-        d, (ql, cl) = self.desc, self._lens(q_lens, ctx_lens)
-        total, words = int(ql.sum()), 0
+        ptr = self._ptr
+        (ql, cl), n, total = _host_lens(q_lens, ctx_lens)
+        words = 0
         if tree_mask is not None:
             if tree_mask.dim() != 2:
                 raise ValueError(f"tree_mask has shape {tuple(tree_mask.shape)}, expected [tokens, words]")
             words = tree_mask.shape[1]
-        self._common(k_cache, v_cache, k_scale, v_scale, block_table, ql.size)
-        n = total * d.num_q_heads * d.head_dim
-        self._tensors(q=(q, self._q_type, n), out=(out, self._q_type, n), tree_mask=(tree_mask, ("int64", "uint64"), total * words))
-        rc = self._lib.ts_tree_attention(self._h, self._stream(stream), _dev_ptr(q), _dev_ptr(k_cache), _dev_ptr(v_cache),
-                                         _dev_ptr(k_scale), _dev_ptr(v_scale), _dev_ptr(block_table), _dev_ptr(tree_mask), words,
-                                         ql.tobytes(), cl.tobytes(), ql.size, sm_scale, _dev_ptr(out))
+        elems = total * self._hq * self._dim
+        rc = self._lib.ts_tree_attention(self._h, self._stream(stream), ptr(q, "q", self._q_type, elems), self._cache_ptr(k_cache, "k_cache"),
+                                         self._cache_ptr(v_cache, "v_cache"), ptr(k_scale, "k_scale", self._f32, self._hkv),
+                                         ptr(v_scale, "v_scale", self._f32, self._hkv),
+                                         ptr(block_table, "block_table", self._i32, n * self._width),
+                                         ptr(tree_mask, "tree_mask", self._i64, total * words), words, ql, cl, n, sm_scale,
+                                         ptr(out, "out", self._q_type, elems))
         if rc != TS_OK:
             self._check(rc)
 
     def kv_move(self, k_cache, v_cache, block_table, src, dst, move_lens, ctx_lens, stream=None):
         """Entries at positions dst take what positions src held; pairs packed by sequence, -1 = no pair."""
-        ml, cl = self._lens(move_lens, ctx_lens)
-        self._common(k_cache, v_cache, None, None, block_table, ml.size)
-        total = int(ml.sum())
-        self._tensors(src=(src, ("int32",), total), dst=(dst, ("int32",), total))
-        rc = self._lib.ts_kv_move(self._h, self._stream(stream), _dev_ptr(k_cache), _dev_ptr(v_cache), _dev_ptr(block_table), _dev_ptr(src),
-                                  _dev_ptr(dst), ml.tobytes(), cl.tobytes(), ml.size)
+        ptr = self._ptr
+        (ml, cl), n, total = _host_lens(move_lens, ctx_lens)
+        rc = self._lib.ts_kv_move(self._h, self._stream(stream), self._cache_ptr(k_cache, "k_cache"), self._cache_ptr(v_cache, "v_cache"),
+                                  ptr(block_table, "block_table", self._i32, n * self._width),
+                                  ptr(src, "src", self._i32, total), ptr(dst, "dst", self._i32, total), ml, cl, n)
         if rc != TS_OK:
             self._check(rc)
 
     def kv_read(self, k_cache, v_cache, k_scale, v_scale, block_table, starts, lens, k_out, v_out, stream=None):
         """Tokens starts .. starts + lens - 1 of every sequence as rows [sum of lens, KV heads, dim]; starts None = 0."""
-        d, (ln, *first) = self.desc, self._lens(*((lens,) if starts is None else (lens, starts)))
-        self._common(k_cache, v_cache, k_scale, v_scale, block_table, ln.size)
-        n = int(ln.sum()) * d.num_kv_heads * d.head_dim
-        self._tensors(k_out=(k_out, self._q_type, n), v_out=(v_out, self._q_type, n))
-        rc = self._lib.ts_kv_read(self._h, self._stream(stream), _dev_ptr(k_cache), _dev_ptr(v_cache), _dev_ptr(k_scale), _dev_ptr(v_scale),
-                                  _dev_ptr(block_table), first[0].tobytes() if first else None, ln.tobytes(), ln.size,
-                                  _dev_ptr(k_out), _dev_ptr(v_out))
+        ptr = self._ptr
+        if starts is None:
+            (ln,), n, total = _host_lens(lens)
+            st = None
+        else:
+            (ln, st), n, total = _host_lens(lens, starts)
+        elems = total * self._hkv * self._dim
+        rc = self._lib.ts_kv_read(self._h, self._stream(stream), self._cache_ptr(k_cache, "k_cache"), self._cache_ptr(v_cache, "v_cache"),
+                                  ptr(k_scale, "k_scale", self._f32, self._hkv), ptr(v_scale, "v_scale", self._f32, self._hkv),
+                                  ptr(block_table, "block_table", self._i32, n * self._width), st, ln, n,
+                                  ptr(k_out, "k_out", self._q_type, elems), ptr(v_out, "v_out", self._q_type, elems))
         if rc != TS_OK:
             self._check(rc)
 

@@ -77,7 +77,7 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a, AppendSeqs
 {
     constexpr int P = D / 2;
     __shared__ f32x2 turn[kPage][P];
-    __shared__ float rows[kPage][D + 1];
+    __shared__ ST rows[kPage][D + 4 / (int)sizeof(ST)];
     const int Hkv = a.geo.Hkv, Hq = a.geo.Hq;
     const int per = Hkv + a.q_slices;
     const int u = a.first_unit + (int)blockIdx.x / per, job = blockIdx.x % per;
@@ -115,7 +115,7 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a, AppendSeqs
     constexpr int X = 16 / (int)sizeof(CT);
     CT* kt = (CT*)a.k_cache + tile;
     CT* vt = (CT*)a.v_cache + tile;
-    const float ks = sizeof(CT) == 1 ? a.k_scale[g] : 1.f, vs = sizeof(CT) == 1 ? a.v_scale[g] : 1.f;
+    [[maybe_unused]] const float ks = sizeof(CT) == 1 ? a.k_scale[g] : 1.f, vs = sizeof(CT) == 1 ? a.v_scale[g] : 1.f;
     for (int i = tid; i < n_tok * P; i += 256) {
         const int p = i % P, t = i / P, slot = r.lo + t;
         const ST* k = (const ST*)a.k + (row0 + t) * a.k_stride + g * D;
@@ -127,12 +127,182 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a, AppendSeqs
     }
     for (int i = tid; i < n_tok * D; i += 256) {
         const int t = i / D, d = i % D;
-        rows[t][d] = load_float((const ST*)a.v + (row0 + t) * a.v_stride + g * D + d);
+        rows[t][d] = ((const ST*)a.v)[(row0 + t) * a.v_stride + g * D + d];
     }
     __syncthreads();
     for (int i = tid; i < n_tok * D; i += 256) {
         const int t = i % n_tok, d = i / n_tok;
-        vt[d * kPage + r.lo + t] = to_cache<CT>(rows[t][d], vs);
+        if constexpr (sizeof(CT) == 1) vt[d * kPage + r.lo + t] = to_cache<CT>(load_float(&rows[t][d]), vs);
+        else vt[d * kPage + r.lo + t] = rows[t][d];                   // same element type: plain copy of the bits
+    }
+}
+
+// The same in 16-byte pieces (bases and strides that allow it; with TS_ROPE_HALF rot_dim / 2 has to be whole pieces).  A thread takes a
+// unit of X pairs (X = elements of a piece) of one token -- two pieces, which hold the pairs' two sides, or X pairs side by side -- and
+// keeps their angles in registers while it goes through the heads; the angles are worked out once per workgroup, in LDS.
+// What bounds it: memory.  34 188 tokens (64/8 heads of 128, bf16): see DESIGN's table for the rate.
+template <typename ST> struct RopePiece { static constexpr int X = 16 / (int)sizeof(ST); float v[X]; };
+template <typename ST>
+__device__ __forceinline__ RopePiece<ST> piece_of(uint4 w)
+{
+    RopePiece<ST> p;
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(ST) == 4) p.v[i] = __uint_as_float(u[i]);
+        else { p.v[2 * i] = __uint_as_float(u[i] << 16); p.v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
+    }
+    return p;
+}
+__device__ __forceinline__ uint32_t pack_pair(float x, float y) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, bf16x2)); }
+template <typename ST>
+__device__ __forceinline__ uint4 words_of(const RopePiece<ST>& p)
+{
+    if constexpr (sizeof(ST) == 4) return make_uint4(__float_as_uint(p.v[0]), __float_as_uint(p.v[1]), __float_as_uint(p.v[2]), __float_as_uint(p.v[3]));
+    else return make_uint4(pack_pair(p.v[0], p.v[1]), pack_pair(p.v[2], p.v[3]), pack_pair(p.v[4], p.v[5]), pack_pair(p.v[6], p.v[7]));
+}
+// Four floats -> four e4m3 bytes, as float_to_e4m3_bits makes them (see encode_e4m3x16 in the append kernels: the hardware conversion
+// agrees with it on every input but NaN once the value is clamped).
+__device__ __forceinline__ uint32_t e4m3_word(float a, float b, float c, float d)
+{
+    const bool nan = !(a == a) | !(b == b) | !(c == c) | !(d == d);
+    int v = __builtin_amdgcn_cvt_pk_fp8_f32(__builtin_amdgcn_fmed3f(a, -448.f, 448.f), __builtin_amdgcn_fmed3f(b, -448.f, 448.f), 0, false);
+    v = __builtin_amdgcn_cvt_pk_fp8_f32(__builtin_amdgcn_fmed3f(c, -448.f, 448.f), __builtin_amdgcn_fmed3f(d, -448.f, 448.f), v, true);
+    if (__any(nan))
+        v = nan ? (int)(float_to_e4m3_bits(a) | float_to_e4m3_bits(b) << 8 | float_to_e4m3_bits(c) << 16 | float_to_e4m3_bits(d) << 24) : v;
+    return (uint32_t)v;
+}
+
+template <typename ST, typename CT, int D>
+__global__ __launch_bounds__(256) void rope_append_vec_kernel(RopeArgs a, AppendSeqs s)
+{
+    constexpr int P = D / 2, X = 16 / (int)sizeof(ST), U = P / X;     // pairs of a head, of a unit; units of a head
+    constexpr int kPad = D + X;                                       // LDS row of V: other banks for the next slot
+    __shared__ __align__(16) f32x2 turn[kPage][P];
+    __shared__ __align__(16) ST vrow[kPage][kPad];
+    const int Hkv = a.geo.Hkv, Hq = a.geo.Hq;
+    const int per = Hkv + a.q_slices;
+    const int u0 = a.first_unit + (int)blockIdx.x / per, job = blockIdx.x % per;
+    const PageRun r = page_run(s, u0);
+    const int tid = threadIdx.x, n_tok = r.hi - r.lo, row0 = r.row_slot0 + r.lo;
+    const int half = a.rope.rot_dim / 2;
+    const bool inter = a.rope.interleaved;
+    // the thread's unit: token t, dims of its two pieces, its heads
+    const int slots = n_tok * U, mine = tid % slots, first = tid / slots, step = 256 / slots;
+    const int t = mine / U, u = mine % U;
+    const bool paired = !inter && u * X < half;                       // two sides of X pairs; else 2 X dims side by side
+    const int d0 = paired || inter ? (inter ? 2 : 1) * u * X : 2 * u * X, d1 = paired ? d0 + half : d0 + X;
+    const bool is_q = job >= Hkv;
+    const int h0 = is_q ? (job - Hkv) * a.heads_per_slice : job, h1 = is_q ? min(h0 + a.heads_per_slice, Hq) : job + 1;
+    const ST* src = is_q ? (const ST*)a.q + (row0 + t) * a.q_stride : (const ST*)a.k + (row0 + t) * a.k_stride;
+    const bool active = first < step;
+    int h = h0 + first;
+    uint4 w0 = {}, w1 = {};
+    if (active && h < h1) {                                           // (on its way while the angles are worked out)
+        w0 = *(const uint4*)(src + h * D + d0);
+        w1 = *(const uint4*)(src + h * D + d1);
+    }
+    if (!is_q) {
+        for (int i = tid; i < n_tok * (D / X); i += 256) {
+            const int tv = i / (D / X), c = i % (D / X);
+            *(uint4*)&vrow[r.lo + tv][c * X] = *(const uint4*)((const ST*)a.v + (row0 + tv) * a.v_stride + job * D + c * X);
+        }
+    }
+    for (int i = tid; i < n_tok * P; i += 256) {
+        const int ti = i / P, p = i % P;
+        const int pos = a.positions ? a.positions[row0 + ti] : r.page_idx * kPage + r.lo + ti;
+        if (p < half) turn[ti][p] = rope_angle(a.rope.turns[p], pos, a.rope.scale);
+    }
+    __syncthreads();
+    f32x2 c[X];
+    bool on[X];
+#pragma unroll
+    for (int e = 0; e < X; ++e) {
+        on[e] = u * X + e < half;
+        c[e] = turn[t][u * X + e];
+    }
+    auto rotate = [&](RopePiece<ST>& x, RopePiece<ST>& y) {
+        if (!inter) {
+#pragma unroll
+            for (int e = 0; e < X; ++e) {
+                const f32x2 v = rotated(x.v[e], y.v[e], c[e], on[e]);
+                x.v[e] = v.x; y.v[e] = v.y;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < X; ++e) {
+                RopePiece<ST>& z = e < X / 2 ? x : y;
+                const int i = 2 * (e % (X / 2));
+                const f32x2 v = rotated(z.v[i], z.v[i + 1], c[e], on[e]);
+                z.v[i] = v.x; z.v[i + 1] = v.y;
+            }
+        }
+    };
+    if (is_q) {
+        if (!active) return;
+        for (; h < h1;) {
+            RopePiece<ST> x = piece_of<ST>(w0), y = piece_of<ST>(w1);
+            const int at = h;
+            h += step;
+            if (h < h1) {                                             // the next head's pieces
+                w0 = *(const uint4*)(src + h * D + d0);
+                w1 = *(const uint4*)(src + h * D + d1);
+            }
+            rotate(x, y);
+            ST* o = (ST*)a.q_out + ((int64_t)(row0 + t) * Hq + at) * D;
+            *(uint4*)(o + d0) = words_of(x);
+            *(uint4*)(o + d1) = words_of(y);
+        }
+        return;
+    }
+    const int g = job;
+    const int64_t tile = tile_elem_base(a.block_table[(int64_t)r.seq * a.geo.max_pages + r.page_idx], Hkv, g, D);
+    CT* kt = (CT*)a.k_cache + tile;
+    CT* vt = (CT*)a.v_cache + tile;
+    if (active && first == 0) {
+        RopePiece<ST> x = piece_of<ST>(w0), y = piece_of<ST>(w1);
+        rotate(x, y);
+        const int slot = r.lo + t;
+        auto store = [&](int d, const RopePiece<ST>& p) {
+            if constexpr (sizeof(CT) == 1) {
+                const float ks = a.k_scale[g];
+                uint32_t w[X / 4];
+#pragma unroll
+                for (int i = 0; i < X / 4; ++i) w[i] = e4m3_word(p.v[4 * i] / ks, p.v[4 * i + 1] / ks, p.v[4 * i + 2] / ks, p.v[4 * i + 3] / ks);
+                *(uint2*)(kt + (d / 16) * 256 + slot * 16 + d % 16) = make_uint2(w[0], w[X / 4 - 1]);
+            } else *(uint4*)(kt + (d / X) * (kPage * X) + slot * X) = words_of(p);
+        };
+        store(d0, x);
+        store(d1, y);
+    }
+    // V: slots fastest in the tile.  A page that is filled whole leaves in 16-byte pieces
+    if (n_tok == kPage) {
+        constexpr int E = 16 / (int)sizeof(CT), PER = kPage / E;      // slots of a piece, pieces of a dim
+        for (int i = tid; i < D * PER; i += 256) {
+            const int d = i / PER, s0 = i % PER * E;
+            if constexpr (sizeof(CT) == 1) {
+                const float vs = a.v_scale[g];
+                uint32_t w[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    w[j] = e4m3_word(load_float(&vrow[4 * j][d]) / vs, load_float(&vrow[4 * j + 1][d]) / vs, load_float(&vrow[4 * j + 2][d]) / vs, load_float(&vrow[4 * j + 3][d]) / vs);
+                *(uint4*)(vt + d * kPage) = make_uint4(w[0], w[1], w[2], w[3]);
+            } else {
+                ST e[E];
+#pragma unroll
+                for (int j = 0; j < E; ++j) e[j] = vrow[s0 + j][d];
+                uint4 w;
+                __builtin_memcpy(&w, e, 16);
+                *(uint4*)(vt + d * kPage + s0) = w;
+            }
+        }
+    } else {
+        for (int i = tid; i < n_tok * D; i += 256) {
+            const int tv = i % n_tok, d = i / n_tok;
+            const ST e = vrow[r.lo + tv][d];
+            if constexpr (sizeof(CT) == 1) vt[d * kPage + r.lo + tv] = to_cache<CT>(load_float(&e), a.v_scale[g]);
+            else vt[d * kPage + r.lo + tv] = e;
+        }
     }
 }
 
@@ -140,7 +310,12 @@ template <typename ST, typename CT>
 static int launch_rope_d(const RopeArgs& a, const AppendSeqs& s, int64_t blocks, hipStream_t st, hipEvent_t done)
 {
     const dim3 grid((unsigned)blocks);
-    if (a.geo.D == 128) return launch_kernel(rope_append_kernel<ST, CT, 128>, grid, dim3(256), st, done, a, s);
+    const bool vec = a.vectors && (a.rope.interleaved || (a.rope.rot_dim / 2) % (16 / (int)sizeof(ST)) == 0);
+    if (a.geo.D == 128) {
+        if (vec) return launch_kernel(rope_append_vec_kernel<ST, CT, 128>, grid, dim3(256), st, done, a, s);
+        return launch_kernel(rope_append_kernel<ST, CT, 128>, grid, dim3(256), st, done, a, s);
+    }
+    if (vec) return launch_kernel(rope_append_vec_kernel<ST, CT, 64>, grid, dim3(256), st, done, a, s);
     return launch_kernel(rope_append_kernel<ST, CT, 64>, grid, dim3(256), st, done, a, s);
 }
 
@@ -165,7 +340,7 @@ int launch_rope_append(const RopeArgs& a, const AppendSeqs& s, int32_t units, vo
     return (int)hipSuccess;
 }
 
-// Reading back: a workgroup takes one page of one KV head through LDS.
+// Reading back: a workgroup takes one page of one KV head.  Element by element, for outputs on any address:
 template <typename CT, typename OT, int D>
 __global__ __launch_bounds__(256) void kv_read_kernel(ReadArgs a, AppendSeqs s)
 {
@@ -194,6 +369,85 @@ __global__ __launch_bounds__(256) void kv_read_kernel(ReadArgs a, AppendSeqs s)
     }
 }
 
+// In 16-byte pieces (16-byte aligned outputs).  K: a thread reads a piece of the tile -- 16 bytes of one token -- and writes it, neighbouring
+// threads neighbouring dims, so that rows leave whole.  V: the tile's pieces (16 bytes of consecutive tokens of one dim) turn into rows in
+// LDS.  What bounds it: memory.
+template <typename CT, typename OT, int D>
+__global__ __launch_bounds__(256) void kv_read_vec_kernel(ReadArgs a, AppendSeqs s)
+{
+    constexpr int X = 16 / (int)sizeof(CT), C = D / X, PER = kPage / X;   // elements of a piece; K pieces of a token; V pieces of a dim
+    constexpr int W = 16 / (int)sizeof(OT), kPad = D + W;
+    constexpr int N = (kPage * C + 255) / 256;                            // pieces of a tile per thread
+    __shared__ __align__(16) OT rows[kPage][kPad];
+    const int Hkv = a.geo.Hkv, tid = threadIdx.x;
+    const int u = a.first_unit + (int)blockIdx.x / Hkv, g = blockIdx.x % Hkv;
+    const PageRun r = page_run(s, u);
+    const int64_t tile = tile_elem_base(a.block_table[(int64_t)r.seq * a.geo.max_pages + r.page_idx], Hkv, g, D);
+    const CT* kt = (const CT*)a.k_cache + tile;
+    const CT* vt = (const CT*)a.v_cache + tile;
+    const int64_t out0 = ((int64_t)r.row_slot0 * Hkv + g) * D;            // (slot 0's row; only slots lo .. hi - 1 are touched)
+    uint4 kw[N], vw[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const int i = tid + 256 * j, slot = i / C, c = i % C;
+        kw[j] = vw[j] = make_uint4(0, 0, 0, 0);
+        if (a.k_out && slot >= r.lo && slot < r.hi) kw[j] = *(const uint4*)(kt + c * (kPage * X) + slot * X);
+        if (a.v_out && i < D * PER) vw[j] = *(const uint4*)(vt + i * X);
+    }
+    auto value = [](uint4 w, int e, float scale) {                        // element e of a piece, e4m3 only
+        const uint32_t u4[4] = {w.x, w.y, w.z, w.w};
+        return e4m3_bits_to_float(u4[e / 4] >> (8 * (e % 4)) & 0xffu) * scale;
+    };
+    if (a.k_out) {
+        OT* out = (OT*)a.k_out + out0;
+        const float scale = sizeof(CT) == 1 ? a.k_scale[g] : 1.f;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int i = tid + 256 * j, slot = i / C, c = i % C;
+            if (slot < r.lo || slot >= r.hi) continue;
+            OT* o = out + (int64_t)slot * Hkv * D + c * X;
+            if constexpr (sizeof(CT) == 1) {
+                uint4 w[2];
+                uint32_t* p = (uint32_t*)w;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) p[e] = pack_pair(value(kw[j], 2 * e, scale), value(kw[j], 2 * e + 1, scale));
+                ((uint4*)o)[0] = w[0];
+                ((uint4*)o)[1] = w[1];
+            } else *(uint4*)o = kw[j];
+        }
+    }
+    if (!a.v_out) return;
+    const float scale = sizeof(CT) == 1 ? a.v_scale[g] : 1.f;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const int i = tid + 256 * j;
+        if (i >= D * PER) continue;
+        const int d = i / PER, s0 = i % PER * X;
+        if constexpr (sizeof(CT) == 1) {
+#pragma unroll
+            for (int e = 0; e < X; ++e) rows[s0 + e][d] = (OT)pack_pair(value(vw[j], e, scale), 0.f);
+        } else {
+            CT e[X];
+            __builtin_memcpy(e, &vw[j], 16);
+#pragma unroll
+            for (int k = 0; k < X; ++k) rows[s0 + k][d] = e[k];
+        }
+    }
+    __syncthreads();
+    OT* out = (OT*)a.v_out + out0;
+    for (int i = tid; i < kPage * (D / W); i += 256) {
+        const int slot = i / (D / W), c = i % (D / W);
+        if (slot >= r.lo && slot < r.hi) *(uint4*)(out + (int64_t)slot * Hkv * D + c * W) = *(const uint4*)&rows[slot][c * W];
+    }
+}
+
+template <typename CT, typename OT, int D>
+static int launch_read_d(const ReadArgs& a, const AppendSeqs& s, dim3 grid, hipStream_t st, hipEvent_t done)
+{
+    if (a.vectors) return launch_kernel(kv_read_vec_kernel<CT, OT, D>, grid, dim3(256), st, done, a, s);
+    return launch_kernel(kv_read_kernel<CT, OT, D>, grid, dim3(256), st, done, a, s);
+}
+
 int launch_kv_read(const ReadArgs& a, const AppendSeqs& s, int32_t units, void* stream, void* done)
 {
     if (a.geo.D != 128 && a.geo.D != 64) return (int)hipErrorInvalidValue;
@@ -206,55 +460,66 @@ int launch_kv_read(const ReadArgs& a, const AppendSeqs& s, int32_t units, void* 
         part.first_unit = (int32_t)u;
         hipStream_t st = (hipStream_t)stream;
         hipEvent_t ev = u + n < units ? nullptr : (hipEvent_t)done;
-        const dim3 grid((unsigned)(n * a.geo.Hkv)), block(256);
+        const dim3 grid((unsigned)(n * a.geo.Hkv));
         int e;
-        if (a.geo.q_dtype == TS_F32)
-            e = d128 ? launch_kernel(kv_read_kernel<float, float, 128>, grid, block, st, ev, part, s) : launch_kernel(kv_read_kernel<float, float, 64>, grid, block, st, ev, part, s);
-        else if (a.geo.kv_dtype == TS_BF16)
-            e = d128 ? launch_kernel(kv_read_kernel<uint16_t, uint16_t, 128>, grid, block, st, ev, part, s) : launch_kernel(kv_read_kernel<uint16_t, uint16_t, 64>, grid, block, st, ev, part, s);
-        else
-            e = d128 ? launch_kernel(kv_read_kernel<uint8_t, uint16_t, 128>, grid, block, st, ev, part, s) : launch_kernel(kv_read_kernel<uint8_t, uint16_t, 64>, grid, block, st, ev, part, s);
+        if (a.geo.q_dtype == TS_F32) e = d128 ? launch_read_d<float, float, 128>(part, s, grid, st, ev) : launch_read_d<float, float, 64>(part, s, grid, st, ev);
+        else if (a.geo.kv_dtype == TS_BF16) e = d128 ? launch_read_d<uint16_t, uint16_t, 128>(part, s, grid, st, ev) : launch_read_d<uint16_t, uint16_t, 64>(part, s, grid, st, ev);
+        else e = d128 ? launch_read_d<uint8_t, uint16_t, 128>(part, s, grid, st, ev) : launch_read_d<uint8_t, uint16_t, 64>(part, s, grid, st, ev);
         if (e != (int)hipSuccess) return e;
     }
     return (int)hipSuccess;
 }
 
-// Moving entries: a workgroup takes one sequence's pairs for one KV head.  Everything is read into LDS before anything is
-// written, so the pairs may overlap and chain in any way.  ET: an integer of the element's size.
+// Moving entries: a workgroup takes one sequence's pairs for one KV head.  Everything is read before anything is written, so the pairs
+// may overlap and chain in any way.  ET: an integer of the element's size.  A path's few entries: what bounds it is the chain of
+// dependent reads (pairs, page ids, entries), which K (in 16-byte pieces) and V go through together.
 template <typename ET, int D>
 __global__ __launch_bounds__(256) void kv_move_kernel(MoveArgs a, MoveSeqs s)
 {
+    constexpr int X = 16 / (int)sizeof(ET), C = D / X;
     __shared__ int from[TS_MAX_MOVES], to[TS_MAX_MOVES];
     __shared__ int64_t src_tile[TS_MAX_MOVES], dst_tile[TS_MAX_MOVES];
-    __shared__ ET held[TS_MAX_MOVES][D + 4 / sizeof(ET)];
+    __shared__ __align__(16) uint4 held_k[TS_MAX_MOVES][C];
+    __shared__ ET held_v[TS_MAX_MOVES][D];
     const int Hkv = a.geo.Hkv;
     const int i = blockIdx.x / Hkv, g = blockIdx.x % Hkv;
     const int first = s.first[i], n = s.first[i + 1] - first, len = s.ctx_len[i];
+    if (n == 0) return;
     const int tid = threadIdx.x;
-    if (tid < n) { from[tid] = a.src[first + tid]; to[tid] = a.dst[first + tid]; }
+    if (tid < n) {
+        from[tid] = a.src[first + tid];
+        to[tid] = a.dst[first + tid];
+    }
     __syncthreads();
     if (tid < n) {
-        bool keep = from[tid] >= 0 && from[tid] < len && to[tid] >= 0 && to[tid] < len;
+        const int f = from[tid], t = to[tid];
+        bool keep = f >= 0 && f < len && t >= 0 && t < len;
         for (int j = tid + 1; keep && j < n; ++j)          // a later pair with the same destination, and a valid source, counts
-            if (to[j] == to[tid] && from[j] >= 0 && from[j] < len) keep = false;
+            if (to[j] == t && from[j] >= 0 && from[j] < len) keep = false;
+        keep = keep && f != t;
         const int32_t* bt = a.block_table + (int64_t)i * a.geo.max_pages;
-        src_tile[tid] = keep ? tile_elem_base(bt[from[tid] >> 4], Hkv, g, D) : -1;
-        dst_tile[tid] = keep ? tile_elem_base(bt[to[tid] >> 4], Hkv, g, D) : -1;
+        src_tile[tid] = keep ? tile_elem_base(bt[f >> 4], Hkv, g, D) : -1;
+        dst_tile[tid] = keep ? tile_elem_base(bt[t >> 4], Hkv, g, D) : -1;
     }
-    constexpr int X = 16 / (int)sizeof(ET);
-    for (int which = 0; which < 2; ++which) {
-        ET* c = (ET*)(which ? a.v_cache : a.k_cache);
-        auto place = [&](int64_t tile, int slot, int d) { return tile + (which ? d * kPage + slot : (d / X) * (kPage * X) + slot * X + d % X); };
-        __syncthreads();
-        for (int e = tid; e < n * D; e += 256) {
-            const int p = e / D, d = e % D;
-            if (src_tile[p] >= 0) held[p][d] = c[place(src_tile[p], from[p] & 15, d)];
-        }
-        __syncthreads();
-        for (int e = tid; e < n * D; e += 256) {
-            const int p = e / D, d = e % D;
-            if (src_tile[p] >= 0) c[place(dst_tile[p], to[p] & 15, d)] = held[p][d];
-        }
+    __syncthreads();
+    ET* kc = (ET*)a.k_cache;
+    ET* vc = (ET*)a.v_cache;
+    for (int e = tid; e < n * C; e += 256) {
+        const int p = e / C, c = e % C;
+        if (src_tile[p] >= 0) held_k[p][c] = *(const uint4*)(kc + src_tile[p] + c * (kPage * X) + (from[p] & 15) * X);
+    }
+    for (int e = tid; e < n * D; e += 256) {
+        const int p = e / D, d = e % D;
+        if (src_tile[p] >= 0) held_v[p][d] = vc[src_tile[p] + d * kPage + (from[p] & 15)];
+    }
+    __syncthreads();
+    for (int e = tid; e < n * C; e += 256) {
+        const int p = e / C, c = e % C;
+        if (src_tile[p] >= 0) *(uint4*)(kc + dst_tile[p] + c * (kPage * X) + (to[p] & 15) * X) = held_k[p][c];
+    }
+    for (int e = tid; e < n * D; e += 256) {
+        const int p = e / D, d = e % D;
+        if (src_tile[p] >= 0) vc[dst_tile[p] + d * kPage + (to[p] & 15)] = held_v[p][d];
     }
 }
 
