@@ -1367,8 +1367,7 @@ extern "C" int ts_rope_kv_append(ts_ctx* c, void* stream, const void* q, int64_t
             row = seqs.seq[n].row0;
             if (units == 0) continue;
             a.block_table = block_table + (int64_t)s0 * c->desc.max_pages_per_seq;
-            a.heads_per_slice = rope_heads_per_slice(c->desc, units, c->opt.n_cu);
-            a.q_slices = q ? (c->desc.num_q_heads + a.heads_per_slice - 1) / a.heads_per_slice : 0;
+            rope_slices(c->desc, row - seqs.seq[0].row0, units, c->opt.n_cu, q != nullptr, &a);
             const hipEvent_t done = last < s0 + n ? op.end : nullptr;
             const hipError_t e = (hipError_t)timed_launch(c, TS_K_APPEND, true, op.st, [&] { return launch_rope_append(a, seqs, (int32_t)units, stream, done); });
             if (e != hipSuccess) return hip_fail(c, e, "rotary append launch");

@@ -305,8 +305,8 @@ struct RopeArgs {
     const float* k_scale; const float* v_scale;
     const int32_t* block_table;        // of the launch's first sequence
     const int32_t* positions;
-    int32_t q_slices;                  // workgroups that share a page's query heads
-    int32_t heads_per_slice;
+    int32_t q_slices, heads_per_slice; // workgroups that share a page's query heads
+    int32_t kv_slices, kv_per_slice;   // ... its KV heads
     int32_t vectors;                   // bases and strides are multiples of 16 bytes
     int32_t first_unit;
     Rope rope;
@@ -388,8 +388,8 @@ inline int32_t tree_groups(int32_t nodes, int32_t G, int32_t rows) { return (int
 constexpr int kTreeWaves = 4;
 constexpr int tree_ring_slots(int slot_bytes) { return 80 * 1024 / slot_bytes < 2 ? 2 : (80 * 1024 / slot_bytes > 4 ? 4 : 80 * 1024 / slot_bytes); }
 
-// Query heads that one workgroup of the rotary append takes of a page's tokens.
-int32_t rope_heads_per_slice(const ts_attn_desc& d, int64_t units, int n_cu);
+// Heads that one workgroup of the rotary append takes of a page's tokens (RopeArgs).
+void rope_slices(const ts_attn_desc& d, int64_t tokens, int64_t units, int n_cu, bool with_q, RopeArgs* a);
 int rope_frequencies(const ts_rope_desc* r, double* freq, double* scale, std::string* err);
 
 // Launchers (defined in the .hip files).  All return a hipError_t cast to int.  done: a hipEvent_t recorded at the end of

@@ -79,7 +79,7 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a, AppendSeqs
     __shared__ f32x2 turn[kPage][P];
     __shared__ ST rows[kPage][D + 4 / (int)sizeof(ST)];
     const int Hkv = a.geo.Hkv, Hq = a.geo.Hq;
-    const int per = Hkv + a.q_slices;
+    const int per = a.kv_slices + a.q_slices;
     const int u = a.first_unit + (int)blockIdx.x / per, job = blockIdx.x % per;
     const PageRun r = page_run(s, u);
     const int tid = threadIdx.x, n_tok = r.hi - r.lo, row0 = r.row_slot0 + r.lo;
@@ -96,8 +96,8 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a, AppendSeqs
         else { x = p; y = p + half; }
     };
     __syncthreads();
-    if (job >= Hkv) {
-        const int h0 = (job - Hkv) * a.heads_per_slice, h1 = min(h0 + a.heads_per_slice, Hq), nh = h1 - h0;
+    if (job >= a.kv_slices) {
+        const int h0 = (job - a.kv_slices) * a.heads_per_slice, h1 = min(h0 + a.heads_per_slice, Hq), nh = h1 - h0;
         for (int i = tid; i < n_tok * nh * P; i += 256) {
             const int p = i % P, h = h0 + i / P % nh, t = i / P / nh;
             const ST* q = (const ST*)a.q + (row0 + t) * a.q_stride + h * D;
@@ -110,9 +110,10 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a, AppendSeqs
         }
         return;
     }
-    const int g = job;
-    const int64_t tile = tile_elem_base(a.block_table[(int64_t)r.seq * a.geo.max_pages + r.page_idx], Hkv, g, D);
+    const int64_t page = a.block_table[(int64_t)r.seq * a.geo.max_pages + r.page_idx];
     constexpr int X = 16 / (int)sizeof(CT);
+    for (int g = job * a.kv_per_slice; g < min((job + 1) * a.kv_per_slice, Hkv); ++g) {
+    const int64_t tile = tile_elem_base(page, Hkv, g, D);
     CT* kt = (CT*)a.k_cache + tile;
     CT* vt = (CT*)a.v_cache + tile;
     [[maybe_unused]] const float ks = sizeof(CT) == 1 ? a.k_scale[g] : 1.f, vs = sizeof(CT) == 1 ? a.v_scale[g] : 1.f;
@@ -135,12 +136,16 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a, AppendSeqs
         if constexpr (sizeof(CT) == 1) vt[d * kPage + r.lo + t] = to_cache<CT>(load_float(&rows[t][d]), vs);
         else vt[d * kPage + r.lo + t] = rows[t][d];                   // same element type: plain copy of the bits
     }
+    __syncthreads();
+    }
 }
 
 // The same in 16-byte pieces (bases and strides that allow it; with TS_ROPE_HALF rot_dim / 2 has to be whole pieces).  A thread takes a
 // unit of X pairs (X = elements of a piece) of one token -- two pieces, which hold the pairs' two sides, or X pairs side by side -- and
 // keeps their angles in registers while it goes through the heads; the angles are worked out once per workgroup, in LDS.
-// What bounds it: memory.  34 188 tokens (64/8 heads of 128, bf16): see DESIGN's table for the rate.
+// What bounds it: memory.  34 188 tokens (64/8 heads of 128, bf16, 1.40 GB read and written): 296 us, 4.7 TB/s of the 5.1 that a large copy
+// reaches.  Stores carry the non-temporal hint (310 us without; 2024 tokens of 40/8 heads 14.1 -> 12.8), loads do not: with it the
+// large append takes 283 us, but inputs that the projection has just left in the caches come from memory (2024 tokens 18.4 us).
 template <typename ST> struct RopePiece { static constexpr int X = 16 / (int)sizeof(ST); float v[X]; };
 template <typename ST>
 __device__ __forceinline__ RopePiece<ST> piece_of(uint4 w)
@@ -181,7 +186,7 @@ __global__ __launch_bounds__(256) void rope_append_vec_kernel(RopeArgs a, Append
     __shared__ __align__(16) f32x2 turn[kPage][P];
     __shared__ __align__(16) ST vrow[kPage][kPad];
     const int Hkv = a.geo.Hkv, Hq = a.geo.Hq;
-    const int per = Hkv + a.q_slices;
+    const int per = a.kv_slices + a.q_slices;
     const int u0 = a.first_unit + (int)blockIdx.x / per, job = blockIdx.x % per;
     const PageRun r = page_run(s, u0);
     const int tid = threadIdx.x, n_tok = r.hi - r.lo, row0 = r.row_slot0 + r.lo;
@@ -192,8 +197,9 @@ __global__ __launch_bounds__(256) void rope_append_vec_kernel(RopeArgs a, Append
     const int t = mine / U, u = mine % U;
     const bool paired = !inter && u * X < half;                       // two sides of X pairs; else 2 X dims side by side
     const int d0 = paired || inter ? (inter ? 2 : 1) * u * X : 2 * u * X, d1 = paired ? d0 + half : d0 + X;
-    const bool is_q = job >= Hkv;
-    const int h0 = is_q ? (job - Hkv) * a.heads_per_slice : job, h1 = is_q ? min(h0 + a.heads_per_slice, Hq) : job + 1;
+    const bool is_q = job >= a.kv_slices;
+    const int h0 = is_q ? (job - a.kv_slices) * a.heads_per_slice : job * a.kv_per_slice;
+    const int h1 = is_q ? min(h0 + a.heads_per_slice, Hq) : min(h0 + a.kv_per_slice, Hkv);
     const ST* src = is_q ? (const ST*)a.q + (row0 + t) * a.q_stride : (const ST*)a.k + (row0 + t) * a.k_stride;
     const bool active = first < step;
     int h = h0 + first;
@@ -202,10 +208,11 @@ __global__ __launch_bounds__(256) void rope_append_vec_kernel(RopeArgs a, Append
         w0 = *(const uint4*)(src + h * D + d0);
         w1 = *(const uint4*)(src + h * D + d1);
     }
-    if (!is_q) {
+    const bool one_head = h1 - h0 == 1;
+    if (!is_q && one_head) {
         for (int i = tid; i < n_tok * (D / X); i += 256) {
             const int tv = i / (D / X), c = i % (D / X);
-            *(uint4*)&vrow[r.lo + tv][c * X] = *(const uint4*)((const ST*)a.v + (row0 + tv) * a.v_stride + job * D + c * X);
+            *(uint4*)&vrow[r.lo + tv][c * X] = *(const uint4*)((const ST*)a.v + (row0 + tv) * a.v_stride + h0 * D + c * X);
         }
     }
     for (int i = tid; i < n_tok * P; i += 256) {
@@ -250,31 +257,48 @@ __global__ __launch_bounds__(256) void rope_append_vec_kernel(RopeArgs a, Append
             }
             rotate(x, y);
             ST* o = (ST*)a.q_out + ((int64_t)(row0 + t) * Hq + at) * D;
-            *(uint4*)(o + d0) = words_of(x);
-            *(uint4*)(o + d1) = words_of(y);
+            store_nt(o + d0, words_of(x));
+            store_nt(o + d1, words_of(y));
         }
         return;
     }
-    const int g = job;
-    const int64_t tile = tile_elem_base(a.block_table[(int64_t)r.seq * a.geo.max_pages + r.page_idx], Hkv, g, D);
-    CT* kt = (CT*)a.k_cache + tile;
-    CT* vt = (CT*)a.v_cache + tile;
-    if (active && first == 0) {
-        RopePiece<ST> x = piece_of<ST>(w0), y = piece_of<ST>(w1);
-        rotate(x, y);
-        const int slot = r.lo + t;
-        auto store = [&](int d, const RopePiece<ST>& p) {
-            if constexpr (sizeof(CT) == 1) {
-                const float ks = a.k_scale[g];
-                uint32_t w[X / 4];
+    const int64_t page = a.block_table[(int64_t)r.seq * a.geo.max_pages + r.page_idx];
+    if (active) {
+        for (; h < h1;) {
+            RopePiece<ST> x = piece_of<ST>(w0), y = piece_of<ST>(w1);
+            const int g = h, slot = r.lo + t;
+            h += step;
+            if (h < h1) {
+                w0 = *(const uint4*)(src + h * D + d0);
+                w1 = *(const uint4*)(src + h * D + d1);
+            }
+            rotate(x, y);
+            CT* kt = (CT*)a.k_cache + tile_elem_base(page, Hkv, g, D);
+            auto store = [&](int d, const RopePiece<ST>& p) {
+                if constexpr (sizeof(CT) == 1) {
+                    const float ks = a.k_scale[g];
+                    uint32_t w[X / 4];
 #pragma unroll
-                for (int i = 0; i < X / 4; ++i) w[i] = e4m3_word(p.v[4 * i] / ks, p.v[4 * i + 1] / ks, p.v[4 * i + 2] / ks, p.v[4 * i + 3] / ks);
-                *(uint2*)(kt + (d / 16) * 256 + slot * 16 + d % 16) = make_uint2(w[0], w[X / 4 - 1]);
-            } else *(uint4*)(kt + (d / X) * (kPage * X) + slot * X) = words_of(p);
-        };
-        store(d0, x);
-        store(d1, y);
+                    for (int i = 0; i < X / 4; ++i) w[i] = e4m3_word(p.v[4 * i] / ks, p.v[4 * i + 1] / ks, p.v[4 * i + 2] / ks, p.v[4 * i + 3] / ks);
+                    *(uint2*)(kt + (d / 16) * 256 + slot * 16 + d % 16) = make_uint2(w[0], w[X / 4 - 1]);
+                } else store_nt(kt + (d / X) * (kPage * X) + slot * X, words_of(p));
+            };
+            store(d0, x);
+            store(d1, y);
+        }
     }
+    if (!one_head) {                                                  // few tokens: V element by element, neighbouring threads neighbouring dims
+        for (int i = tid; i < n_tok * (h1 - h0) * D; i += 256) {
+            const int d = i % D, g = h0 + i / D % (h1 - h0), tv = i / D / (h1 - h0);
+            const ST e = ((const ST*)a.v)[(row0 + tv) * a.v_stride + g * D + d];
+            CT* vt = (CT*)a.v_cache + tile_elem_base(page, Hkv, g, D) + d * kPage + r.lo + tv;
+            if constexpr (sizeof(CT) == 1) *vt = to_cache<CT>(load_float(&e), a.v_scale[g]);
+            else *vt = e;
+        }
+        return;
+    }
+    const int g = h0;
+    CT* vt = (CT*)a.v_cache + tile_elem_base(page, Hkv, g, D);
     // V: slots fastest in the tile.  A page that is filled whole leaves in 16-byte pieces
     if (n_tok == kPage) {
         constexpr int E = 16 / (int)sizeof(CT), PER = kPage / E;      // slots of a piece, pieces of a dim
@@ -286,14 +310,14 @@ __global__ __launch_bounds__(256) void rope_append_vec_kernel(RopeArgs a, Append
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     w[j] = e4m3_word(load_float(&vrow[4 * j][d]) / vs, load_float(&vrow[4 * j + 1][d]) / vs, load_float(&vrow[4 * j + 2][d]) / vs, load_float(&vrow[4 * j + 3][d]) / vs);
-                *(uint4*)(vt + d * kPage) = make_uint4(w[0], w[1], w[2], w[3]);
+                store_nt(vt + d * kPage, make_uint4(w[0], w[1], w[2], w[3]));
             } else {
                 ST e[E];
 #pragma unroll
                 for (int j = 0; j < E; ++j) e[j] = vrow[s0 + j][d];
                 uint4 w;
                 __builtin_memcpy(&w, e, 16);
-                *(uint4*)(vt + d * kPage + s0) = w;
+                store_nt(vt + d * kPage + s0, w);
             }
         }
     } else {
@@ -323,7 +347,7 @@ int launch_rope_append(const RopeArgs& a, const AppendSeqs& s, int32_t units, vo
 {
     if (a.geo.D != 128 && a.geo.D != 64) return (int)hipErrorInvalidValue;
     RopeArgs part = a;
-    const int per = a.geo.Hkv + a.q_slices;
+    const int per = a.kv_slices + a.q_slices;
     const int64_t most = kMaxWorkgroups / per;
     if (most < 1) return (int)hipErrorInvalidValue;
     for (int64_t u = 0; u < units; u += most) {
@@ -371,7 +395,8 @@ __global__ __launch_bounds__(256) void kv_read_kernel(ReadArgs a, AppendSeqs s)
 
 // In 16-byte pieces (16-byte aligned outputs).  K: a thread reads a piece of the tile -- 16 bytes of one token -- and writes it, neighbouring
 // threads neighbouring dims, so that rows leave whole.  V: the tile's pieces (16 bytes of consecutive tokens of one dim) turn into rows in
-// LDS.  What bounds it: memory.
+// LDS.  What bounds it: memory.  108 951 tokens of an e4m3 cache (64/8 heads of 128, 0.22 GB read, 0.45 written): 129 us, 5.2 TB/s, 166
+// without the non-temporal hint on the stores; loads with it 154.
 template <typename CT, typename OT, int D>
 __global__ __launch_bounds__(256) void kv_read_vec_kernel(ReadArgs a, AppendSeqs s)
 {
@@ -411,9 +436,9 @@ __global__ __launch_bounds__(256) void kv_read_vec_kernel(ReadArgs a, AppendSeqs
                 uint32_t* p = (uint32_t*)w;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) p[e] = pack_pair(value(kw[j], 2 * e, scale), value(kw[j], 2 * e + 1, scale));
-                ((uint4*)o)[0] = w[0];
-                ((uint4*)o)[1] = w[1];
-            } else *(uint4*)o = kw[j];
+                store_nt(o, w[0]);
+                store_nt(o + 8, w[1]);
+            } else store_nt(o, kw[j]);
         }
     }
     if (!a.v_out) return;
@@ -437,7 +462,7 @@ __global__ __launch_bounds__(256) void kv_read_vec_kernel(ReadArgs a, AppendSeqs
     OT* out = (OT*)a.v_out + out0;
     for (int i = tid; i < kPage * (D / W); i += 256) {
         const int slot = i / (D / W), c = i % (D / W);
-        if (slot >= r.lo && slot < r.hi) *(uint4*)(out + (int64_t)slot * Hkv * D + c * W) = *(const uint4*)&rows[slot][c * W];
+        if (slot >= r.lo && slot < r.hi) store_nt(out + (int64_t)slot * Hkv * D + c * W, *(const uint4*)&rows[slot][c * W]);
     }
 }
 
@@ -472,7 +497,9 @@ int launch_kv_read(const ReadArgs& a, const AppendSeqs& s, int32_t units, void* 
 
 // Moving entries: a workgroup takes one sequence's pairs for one KV head.  Everything is read before anything is written, so the pairs
 // may overlap and chain in any way.  ET: an integer of the element's size.  A path's few entries: what bounds it is the chain of
-// dependent reads (pairs, page ids, entries), which K (in 16-byte pieces) and V go through together.
+// dependent reads (pairs, page ids, entries), which K (in 16-byte pieces) and V go through together, and in large batches the lines of
+// the V tiles, all of which an entry touches (one element per dim): 256 paths of 1-9 tokens over 8 KV heads of 128 dims, e4m3, 8.0 us (9.9
+// with K and V one after the other; 8.7 with the pairs looked at by every wave, without an exchange through LDS).
 template <typename ET, int D>
 __global__ __launch_bounds__(256) void kv_move_kernel(MoveArgs a, MoveSeqs s)
 {
