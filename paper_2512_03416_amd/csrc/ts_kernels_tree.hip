@@ -591,7 +591,7 @@ static int launch_tree_d(const TreeArgs& a, const TreeSeqs& s, int64_t items, hi
     const dim3 grid((unsigned)items), block(64 * kTrWaves);
     if (a.rows == 64) return launch_kernel(tree_kernel<KT, D, 2>, grid, block, st, done, a, s);
     if (a.rows == 128) return launch_kernel(tree_kernel<KT, D, 4>, grid, block, st, done, a, s);
-    if constexpr (sizeof(KT) != 4) {
+    if constexpr (sizeof(KT) != 4 || D == 64) {
         if (a.rows == 32) return launch_kernel(tree_kernel<KT, D, 1>, grid, block, st, done, a, s);
     }
     return (int)hipErrorInvalidValue;

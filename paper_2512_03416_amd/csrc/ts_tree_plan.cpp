@@ -81,26 +81,34 @@ void rope_slices(const ts_attn_desc& d, int64_t tokens, int64_t units, int n_cu,
     a->q_slices = with_q ? (d.num_q_heads + heads - 1) / heads : 0;
 }
 
-// Times of the tree kernel in us, measured, from which the cuts are chosen.  They need to be right to a third or so.
+// Times of the tree kernel in us, measured, from which its rows per workgroup and its cuts are chosen.
 struct TreeTimes {
     double page_alone;                 // a page (K and V of one KV head) of a workgroup that has the GPU to itself: bound by latency, in
-                                       // proportion to the waves that share it (64-row workgroups take two pages at a time)
-    double page_full;                  // the same with a workgroup in every place: bound by the matrix products and the softmax
+                                       // proportion to the waves that share it (64-row workgroups take two pages at a time, 32-row ones four)
+    double page_full;                  // the same with a workgroup in every place: bound by the matrix products, the softmax and the LDS
     double page_read;                  // a page read from HBM, by whichever of its groups of rows comes first
     int64_t places;                    // workgroups resident at once
     double start, round;               // launch, page ids, queries, first copies, last stores; of a later workgroup in the same place
     double merge, merge_row;           // merge launch, and a partial row written and read again
 };
+static int tree_round(int rows) { return 2 * kTreeWaves * 32 / rows; }     // pages that a workgroup's waves take in turn
+static bool tree_rows_fit(const ts_attn_desc& d, int rows)             // (fp32 with 128 dims: a ring for four waves' own keys exceeds the LDS)
+{
+    return rows > 32 || d.q_dtype != TS_F32 || d.head_dim == 64;
+}
 static TreeTimes tree_times(const ts_attn_desc& d, int rows, int n_cu)
 {
     const int elem = d.kv_dtype == TS_F32 ? 4 : (d.kv_dtype == TS_BF16 ? 2 : 1);
-    const int slot = 2 * kTreeWaves * 32 / rows * 2 * kPage * d.head_dim * elem;
+    const int slot = tree_round(rows) * 2 * kPage * d.head_dim * elem;
     const double dims = d.head_dim / 128.0, math = d.q_dtype == TS_F32 ? 8.0 : 1.0;
     TreeTimes t;
-    t.places = (int64_t)n_cu * std::max(1, std::min(2, 160 * 1024 / (slot * tree_ring_slots(slot))));
-    const double per_cu = (double)t.places / n_cu;
+    const int per_cu = std::max(1, std::min(2, 160 * 1024 / (slot * tree_ring_slots(slot))));
+    t.places = (int64_t)n_cu * per_cu;
     t.page_alone = 0.36 * rows / 128 * (0.3 + 0.7 * dims) * math;
-    t.page_full = 0.27 * per_cu * rows / 128 * dims * math;    // 0.54 with 128 rows and two workgroups per CU
+    // 32 trees of 64 nodes over 8 Ki tokens (64/8 heads of 128): bf16 594 us with 128 rows, 639 with 64, 971 with 32 (one workgroup per CU, and
+    // L2 reads of 17 TB/s); 8 trees of 100-128 nodes over 2-9 Ki, e4m3: 219, 191, 203
+    const bool e4m3 = elem == 1;
+    t.page_full = (rows == 32 ? (per_cu == 1 ? 0.118 : (e4m3 ? 0.155 : 0.16)) : (rows == 64 ? (per_cu == 1 ? 0.2 : (e4m3 ? 0.28 : 0.31)) : (per_cu == 1 ? 0.36 : (e4m3 ? 0.57 : 0.55)))) * dims * math;
     t.page_read = 2.0 * kPage * d.head_dim * elem / 6.2e6;     // 6.2 TB/s
     t.start = 5.0;
     t.round = 2.5;
@@ -109,73 +117,85 @@ static TreeTimes tree_times(const ts_attn_desc& d, int rows, int n_cu)
     return t;
 }
 
-// Uncut, a scan writes no partial results, and the longest scans come first, so that a batch with a workgroup or more for every place
+// Rows per workgroup: 128 share every copied page four ways; with 32, each wave copies and scans keys of its own and waits for no other,
+// which is faster wherever L2 and HBM keep up (4 trees of 7-26 nodes over 0.5-2.5 Ki tokens, 32/8 heads, 17.0 us with 32 rows, 19.6 with 128).
+// Cuts: uncut, a scan writes no partial results, and the longest scans come first, so that a batch with a workgroup or more for every place
 // comes out even by itself: 32 trees of 32-64 nodes over 1-8 Ki tokens (64/8 heads) take 284 us uncut, 297 in ranges of at most 384
 // pages, 317 in ranges of 192.  Smaller batches are cut until the workgroups fill the places: 8 trees of 30 nodes over 4000 tokens
-// (32/8 heads) 92 us uncut, 38 in ranges of 32 to 64 pages, 54 in ranges of 16 (most of it partial results).  Ranges of a sequence are of
-// one length.
+// (32/8 heads, 128 rows) 92 us uncut, 38 in ranges of 32 to 64 pages, 54 in ranges of 16 (most of it partial results).  Ranges of a sequence
+// are of one length.  Both are taken from the times above, which come within a tenth of the best choice on these batches and eight more.
 void plan_tree(const ts_attn_desc& d, const int32_t* q_lens, const int32_t* ctx_lens, int num_seqs, int n_cu, TreePlan* plan)
 {
     const int32_t G = d.num_q_heads / d.num_kv_heads, Hkv = d.num_kv_heads;
     plan->seqs.clear();
-    int64_t most = 0, row = 0, total = 0;
+    int64_t most = 0, row = 0, scans = 0;                      // most rows of a sequence; pages of all scans
     int32_t longest = 0;
     auto pages_of = [](const TreeSeq& s) { return (s.prefix + s.n_nodes + kPage - 1) / kPage; };
     for (int s = 0; s < num_seqs; ++s) {
         if (q_lens[s] > 0) {
             most = std::max<int64_t>(most, (int64_t)q_lens[s] * G);
             plan->seqs.push_back(TreeSeq{s, (int32_t)row, q_lens[s], ctx_lens[s] - q_lens[s], 0, 1, 0, 0, 0});
-            longest = std::max(longest, pages_of(plan->seqs.back()));
+            const int32_t pages = pages_of(plan->seqs.back());
+            longest = std::max(longest, pages);
+            scans += pages;
         }
         row += q_lens[s];
     }
-    plan->rows = most <= 32 && d.q_dtype != TS_F32 ? 32 : (most <= 64 ? 64 : 128);
-    const int32_t round = 2 * kTreeWaves * 32 / plan->rows;    // pages that a workgroup's waves take in turn
-    auto groups_of = [&](const TreeSeq& s) { return tree_groups(s.n_nodes, G, plan->rows); };
-    int64_t scans = 0;                                         // pages of all scans, and of all scans' groups of rows
-    for (const TreeSeq& s : plan->seqs) { scans += pages_of(s); total += (int64_t)pages_of(s) * groups_of(s); }
-    const TreeTimes t = tree_times(d, plan->rows, n_cu);
-    auto cut_to = [&](int32_t L) {                             // ranges of at most L pages (a multiple of round)
+    auto cut_to = [&](int32_t L, int round) {                  // ranges of at most L pages, a multiple of round
         for (TreeSeq& s : plan->seqs) {
-            const int32_t pages = pages_of(s), parts = (pages + L - 1) / L;
-            s.part_pages = ((pages + parts - 1) / parts + round - 1) / round * round;
-            s.parts = (pages + s.part_pages - 1) / s.part_pages;
+            const int32_t pages = pages_of(s);
+            s.parts = 1;
+            s.part_pages = L;
+            if (pages > L) {
+                const int32_t parts = (pages + L - 1) / L;
+                s.part_pages = ((pages + parts - 1) / parts + round - 1) / round * round;
+                s.parts = (pages + s.part_pages - 1) / s.part_pages;
+            }
         }
     };
-    const int32_t whole = (longest + round - 1) / round * round;
     std::vector<std::pair<int32_t, int32_t>> ranges;
-    int32_t best = whole;
+    plan->rows = 128;
+    int32_t best = 0;
     double best_time = 0.0;
-    for (int32_t L = whole; L >= round; L = std::min((L / 4 * 3 + round - 1) / round * round, L - round)) {
-        int64_t items = 0, rows = 0;
-        int32_t len = 0;
-        cut_to(L);
-        for (const TreeSeq& s : plan->seqs) {
-            items += (int64_t)s.parts * Hkv * groups_of(s);
-            len = std::max(len, std::min(s.part_pages, pages_of(s)));
-            if (s.parts > 1) rows += (int64_t)s.parts * s.n_nodes * d.num_q_heads;
+    for (int rows_wg = 128; rows_wg >= 32; rows_wg /= 2) {
+        if (!tree_rows_fit(d, rows_wg)) break;
+        if (rows_wg > 32 && tree_rows_fit(d, rows_wg / 2) && most <= rows_wg / 2) continue;   // (half of the rows would be empty everywhere)
+        const TreeTimes t = tree_times(d, rows_wg, n_cu);
+        const int32_t round = tree_round(rows_wg), whole = (longest + round - 1) / round * round;
+        auto groups_of = [&](const TreeSeq& s) { return tree_groups(s.n_nodes, G, rows_wg); };
+        int64_t total = 0;                                     // pages of all scans' groups of rows
+        for (const TreeSeq& s : plan->seqs) total += (int64_t)pages_of(s) * groups_of(s);
+        for (int32_t L = whole; L >= round; L = std::min((L / 4 * 3 + round - 1) / round * round, L - round)) {
+            int64_t items = 0, rows = 0;
+            int32_t len = 0;
+            cut_to(L, round);
+            for (const TreeSeq& s : plan->seqs) {
+                items += (int64_t)s.parts * Hkv * groups_of(s);
+                len = std::max(len, std::min(s.part_pages, pages_of(s)));
+                if (s.parts > 1) rows += (int64_t)s.parts * s.n_nodes * d.num_q_heads;
+            }
+            if (rows > kTreePartRows) break;                   // (shorter ranges have more of them)
+            const double fill = std::min(1.0, (double)items / t.places), page = std::max(t.page_alone, t.page_full * fill);
+            // the longest range, or all of them on the places they have (one behind the other, the shortest last, leaves a little
+            // unevenness), or HBM
+            double time = std::max(len * t.page_alone, (double)total * Hkv / std::min<int64_t>(items, t.places) * page);
+            if (items > n_cu && items <= t.places) {           // the longest ranges share their CUs with those from number n_cu on
+                ranges.clear();
+                for (const TreeSeq& s : plan->seqs) ranges.push_back({std::min(s.part_pages, pages_of(s)), s.parts * Hkv * groups_of(s)});
+                std::sort(ranges.begin(), ranges.end(), std::greater<>());
+                int64_t before = 0;
+                size_t k = 0;
+                while (k + 1 < ranges.size() && before + ranges[k].second <= n_cu) before += ranges[k++].second;
+                time = std::max(time, 0.85 * (len * t.page_alone + ranges[k].first * std::max(0.0, t.page_full - t.page_alone)));
+            }
+            if (items > t.places) time += 0.15 * page * total * Hkv / items + ((double)items / t.places - 1.0) * t.round;
+            time = t.start + std::max(time, scans * Hkv * t.page_read);
+            if (rows > 0) time += t.merge + rows * t.merge_row;
+            if (best == 0 || time < best_time) { plan->rows = rows_wg; best = L; best_time = time; }
+            if (items > 4 * t.places) break;
         }
-        if (rows > kTreePartRows) break;                       // (shorter ranges have more of them)
-        const double fill = std::min(1.0, (double)items / t.places), page = std::max(t.page_alone, t.page_full * fill);
-        // the longest range, or all of them on the places they have (one behind the other, the shortest last, leaves a little
-        // unevenness), or HBM
-        double time = std::max(len * t.page_alone, (double)total * Hkv / std::min<int64_t>(items, t.places) * page);
-        if (items > n_cu && items <= t.places) {               // the longest ranges share their CUs with those from number n_cu on
-            ranges.clear();
-            for (const TreeSeq& s : plan->seqs) ranges.push_back({std::min(s.part_pages, pages_of(s)), s.parts * Hkv * groups_of(s)});
-            std::sort(ranges.begin(), ranges.end(), std::greater<>());
-            int64_t before = 0;
-            size_t k = 0;
-            while (k + 1 < ranges.size() && before + ranges[k].second <= n_cu) before += ranges[k++].second;
-            time = std::max(time, 0.85 * (len * t.page_alone + ranges[k].first * std::max(0.0, t.page_full - t.page_alone)));
-        }
-        if (items > t.places) time += 0.15 * page * total * Hkv / items + ((double)items / t.places - 1.0) * t.round;
-        time = t.start + std::max(time, scans * Hkv * t.page_read);
-        if (rows > 0) time += t.merge + rows * t.merge_row;
-        if (L == whole || time < best_time) { best = L; best_time = time; }
-        if (items > 4 * t.places) break;
     }
-    cut_to(best);
+    cut_to(std::max(best, 1), tree_round(plan->rows));
     plan->part_rows = 0;
     for (TreeSeq& s : plan->seqs)
         if (s.parts > 1) {
