@@ -167,8 +167,8 @@ int ts_mixed_paged_attention_noalloc(ts_ctx *ctx, void *stream,
  *
  * Conventions as above, and: these calls allocate nothing on the device but ts_tree_attention's scratch (see
  * ts_reserve_tree), use no pinned memory and keep no lists on the device, so all of them may be captured into a graph; a
- * captured call fixes the HOST arrays' values.  A context orders its eager calls among streams; the replays of a graph are
- * ordered by the caller.  "kernel_timing" counts the append, move and read under TS_K_APPEND, the tree attention under
+ * captured call fixes the HOST arrays' values.  A context orders its eager calls among streams; the replays of its graphs,
+ * which share its scratch, are ordered by the caller.  k_cache and v_cache must be 16-byte aligned.  "kernel_timing" counts the append, move and read under TS_K_APPEND, the tree attention under
  * TS_K_DECODE and its merge under TS_K_COMBINE (eager calls only); "validate_block_table" is honoured, but refused under
  * capture (TS_ERR_UNSUPPORTED).  None of them touches the velocity counters. */
 
@@ -234,7 +234,7 @@ int ts_rope_kv_append(ts_ctx *ctx, void *stream,
  *   tree_mask : DEV uint64 [T, mask_words]: bit j % 64 of word j / 64 of row (s, i) = node i sees node j; bits from
  *               q_lens[s] on are ignored.  A node that sees no key at all gets zeros.  NULL = chains: node i sees nodes 0 .. i
  *               (mask_words is not read)
- *   other arguments as in ts_mixed_paged_attention; q [T, Hq, D] and out [T, Hq, D] must be 16-byte aligned
+ *   other arguments as in ts_mixed_paged_attention; q [T, Hq, D] and out [T, Hq, D] must be 16-byte aligned and not overlap
  * What a row does not see has no influence on it, whatever its value (infinities and NaN included).  A row whose visible
  * scores are all -inf is NaN.  Softmax statistics and sums are held in single precision, the weights enter the second
  * product in q_dtype.  Results are run-to-run identical.
@@ -262,7 +262,8 @@ int ts_tree_masks(const int32_t *parents, const int32_t *q_lens, int num_seqs, i
  *   src, dst : DEV int32 [sum of move_lens]
  *   move_lens, ctx_lens : HOST int32 [S]; a pair with a position outside [0, ctx_lens[s]) is skipped (-1 as padding); of
  *                         several pairs with one dst the last counts
- * Entries that move into a page that another sequence shares move for that sequence too.
+ * Entries that move into a page that another sequence shares move for that sequence too; one call must not write an entry for
+ * one sequence that it reads or writes for another.
  * Errors: TS_ERR_INVALID_ARG for null pointers, negative lengths, ctx_lens beyond the table; TS_ERR_UNSUPPORTED for more than
  * TS_MAX_MOVES pairs of a sequence. */
 #define TS_MAX_MOVES 64

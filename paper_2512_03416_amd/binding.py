@@ -287,16 +287,16 @@ def tree_masks(parents, q_lens, mask_words: int = 0):
 _raw_stream = None
 
 
-def _current_stream() -> int:
-    """Handle of torch's current stream.  torch.cuda.current_stream() builds a Stream object for it (2.9 us a call); the
+def _current_stream(device=None) -> int:
+    """Handle of torch's current stream on a GPU (None = the current one).  torch.cuda.current_stream() builds a Stream object for it (2.9 us a call); the
     function under it returns the handle itself (0.1 us)."""
     global _raw_stream
     if _raw_stream is None:
         import torch
         torch.cuda.current_stream()                        # initialises the GPU if nothing has yet
-        get, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
-        _raw_stream = (lambda: get(device())) if get and device else (lambda: torch.cuda.current_stream().cuda_stream)
-    return _raw_stream()
+        get, current = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+        _raw_stream = (lambda d: get(current() if d is None else d)) if get and current else (lambda d: torch.cuda.current_stream(d).cuda_stream)
+    return _raw_stream(device)
 
 
 class Context:
@@ -337,9 +337,9 @@ class Context:
             raise TokenScaleError(rc, self.last_error())
 
     @staticmethod
-    def _stream(stream) -> int:
+    def _stream(stream, device=None) -> int:
         if stream is None:
-            return _current_stream()
+            return _current_stream(device)
         if isinstance(stream, int):
             return stream
         return stream.cuda_stream
@@ -415,6 +415,8 @@ class Context:
         row, head, one = t.stride()
         if one != 1 or (head != dim and heads > 1):
             raise ValueError(f"{name}: a row's heads and dims must be packed")
+        if total > 1 and row < heads * dim:                # (an expanded tensor's 0 would be taken for packed rows)
+            raise ValueError(f"{name}: rows {row} elements apart overlap")
         return t.data_ptr(), row if total > 1 else 0
 
     def _cache_ptr(self, t, name: str) -> int:
@@ -436,7 +438,7 @@ class Context:
         """q, k_new, v_new: [T, heads, dim], rows may be strided (slices of one projection's output); q_out packed, may be q."""
         ptr, rows, hq, hkv = self._ptr, self._rows, self._hq, self._hkv
         (ql, cl), n, total = _host_lens(q_lens, ctx_lens)
-        rc = self._lib.ts_rope_kv_append(self._h, self._stream(stream), *rows(q, "q", hq, total), *rows(k_new, "k_new", hkv, total),
+        rc = self._lib.ts_rope_kv_append(self._h, self._stream(stream, self.device), *rows(q, "q", hq, total), *rows(k_new, "k_new", hkv, total),
                                          *rows(v_new, "v_new", hkv, total), ptr(q_out, "q_out", self._q_type, total * hq * self._dim),
                                          self._cache_ptr(k_cache, "k_cache"), self._cache_ptr(v_cache, "v_cache"),
                                          ptr(k_scale, "k_scale", self._f32, hkv), ptr(v_scale, "v_scale", self._f32, hkv),
@@ -460,7 +462,7 @@ class Context:
                 raise ValueError(f"tree_mask has shape {tuple(tree_mask.shape)}, expected [tokens, words]")
             words = tree_mask.shape[1]
         elems = total * self._hq * self._dim
-        rc = self._lib.ts_tree_attention(self._h, self._stream(stream), ptr(q, "q", self._q_type, elems), self._cache_ptr(k_cache, "k_cache"),
+        rc = self._lib.ts_tree_attention(self._h, self._stream(stream, self.device), ptr(q, "q", self._q_type, elems), self._cache_ptr(k_cache, "k_cache"),
                                          self._cache_ptr(v_cache, "v_cache"), ptr(k_scale, "k_scale", self._f32, self._hkv),
                                          ptr(v_scale, "v_scale", self._f32, self._hkv),
                                          ptr(block_table, "block_table", self._i32, n * self._width),
@@ -473,7 +475,7 @@ class Context:
         """Entries at positions dst take what positions src held; pairs packed by sequence, -1 = no pair."""
         ptr = self._ptr
         (ml, cl), n, total = _host_lens(move_lens, ctx_lens)
-        rc = self._lib.ts_kv_move(self._h, self._stream(stream), self._cache_ptr(k_cache, "k_cache"), self._cache_ptr(v_cache, "v_cache"),
+        rc = self._lib.ts_kv_move(self._h, self._stream(stream, self.device), self._cache_ptr(k_cache, "k_cache"), self._cache_ptr(v_cache, "v_cache"),
                                   ptr(block_table, "block_table", self._i32, n * self._width),
                                   ptr(src, "src", self._i32, total), ptr(dst, "dst", self._i32, total), ml, cl, n)
         if rc != TS_OK:
@@ -488,7 +490,7 @@ class Context:
         else:
             (ln, st), n, total = _host_lens(lens, starts)
         elems = total * self._hkv * self._dim
-        rc = self._lib.ts_kv_read(self._h, self._stream(stream), self._cache_ptr(k_cache, "k_cache"), self._cache_ptr(v_cache, "v_cache"),
+        rc = self._lib.ts_kv_read(self._h, self._stream(stream, self.device), self._cache_ptr(k_cache, "k_cache"), self._cache_ptr(v_cache, "v_cache"),
                                   ptr(k_scale, "k_scale", self._f32, self._hkv), ptr(v_scale, "v_scale", self._f32, self._hkv),
                                   ptr(block_table, "block_table", self._i32, n * self._width), st, ln, n,
                                   ptr(k_out, "k_out", self._q_type, elems), ptr(v_out, "v_out", self._q_type, elems))

@@ -1296,6 +1296,16 @@ int64_t op_seqs(AppendSeqs* out, const int32_t* lens, const int32_t* prefixes, i
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
+// (tiles are moved in 16-byte pieces)
+int check_op_caches(ts_ctx* c, const void* k_cache, const void* v_cache)
+{
+    if (!aligned16(k_cache) || !aligned16(v_cache)) return fail(c, TS_ERR_INVALID_ARG, "k_cache / v_cache is not 16-byte aligned");
+    return TS_OK;
+}
+// Pages of a length up to INT32_MAX.
+int32_t pages_up_to(int64_t len) { return (int32_t)((len + kPage - 1) / kPage); }
+constexpr int32_t kOpMaxLen = INT32_MAX - 1023;            // (a tree's key numbers run on to the end of the last round of pages)
+
 }  // namespace
 
 extern "C" int ts_set_rope(ts_ctx* c, const ts_rope_desc* rope)
@@ -1328,6 +1338,8 @@ extern "C" int ts_rope_kv_append(ts_ctx* c, void* stream, const void* q, int64_t
         c->err.clear();
         int rc = check_common(c, k_cache, v_cache, k_scale, v_scale, block_table, q_lens, ctx_lens, num_seqs);
         if (rc != TS_OK) return rc;
+        rc = check_op_caches(c, k_cache, v_cache);
+        if (rc != TS_OK) return rc;
         if (c->rope.rot_dim == 0) return fail(c, TS_ERR_INVALID_ARG, "no rotary positions set (ts_set_rope)");
         const int64_t qw = (int64_t)c->desc.num_q_heads * c->desc.head_dim, kw = (int64_t)c->desc.num_kv_heads * c->desc.head_dim;
         if ((q_stride != 0 && q_stride < qw) || (k_stride != 0 && k_stride < kw) || (v_stride != 0 && v_stride < kw))
@@ -1342,7 +1354,7 @@ extern "C" int ts_rope_kv_append(ts_ctx* c, void* stream, const void* q, int64_t
         Op op{c, (hipStream_t)stream};
         rc = op.begin();
         if (rc != TS_OK) return rc;
-        rc = check_op_pages(op, block_table, num_seqs, [&](int s) { return (ctx_lens[s] + kPage - 1) / kPage; });
+        rc = check_op_pages(op, block_table, num_seqs, [&](int s) { return pages_up_to(ctx_lens[s]); });
         if (rc != TS_OK) return rc;
         RopeArgs a{};
         a.geo = geometry_of(c->desc);
@@ -1403,9 +1415,13 @@ extern "C" int ts_tree_attention(ts_ctx* c, void* stream, const void* q, const v
         c->err.clear();
         int rc = check_common(c, k_cache, v_cache, k_scale, v_scale, block_table, q_lens, ctx_lens, num_seqs);
         if (rc != TS_OK) return rc;
+        rc = check_op_caches(c, k_cache, v_cache);
+        if (rc != TS_OK) return rc;
         if (!(sm_scale == sm_scale)) return fail(c, TS_ERR_INVALID_ARG, "sm_scale is NaN");
         int64_t total = 0;
+        if ((uintptr_t)tree_mask & 7) return fail(c, TS_ERR_INVALID_ARG, "tree_mask is not 8-byte aligned");
         for (int s = 0; s < num_seqs; ++s) {
+            if (ctx_lens[s] > kOpMaxLen) return fail(c, TS_ERR_UNSUPPORTED, "sequence " + std::to_string(s) + ": ctx_len is too large");
             if (q_lens[s] > TS_TREE_MAX_NODES)
                 return fail(c, TS_ERR_UNSUPPORTED, "sequence " + std::to_string(s) + ": " + std::to_string(q_lens[s]) + " nodes, at most " +
                                                        std::to_string(TS_TREE_MAX_NODES));
@@ -1429,7 +1445,7 @@ extern "C" int ts_tree_attention(ts_ctx* c, void* stream, const void* q, const v
             rc = ts_reserve_tree(c);
             if (rc != TS_OK) return rc;
         }
-        rc = check_op_pages(op, block_table, num_seqs, [&](int s) { return q_lens[s] > 0 ? (ctx_lens[s] + kPage - 1) / kPage : 0; });
+        rc = check_op_pages(op, block_table, num_seqs, [&](int s) { return q_lens[s] > 0 ? pages_up_to(ctx_lens[s]) : 0; });
         if (rc != TS_OK) return rc;
         TreeArgs a{};
         a.geo = geometry_of(c->desc);
@@ -1480,6 +1496,8 @@ extern "C" int ts_kv_move(ts_ctx* c, void* stream, void* k_cache, void* v_cache,
         c->err.clear();
         if (num_seqs < 0) return fail(c, TS_ERR_INVALID_ARG, "num_seqs is negative");
         if (!k_cache || !v_cache) return fail(c, TS_ERR_INVALID_ARG, "k_cache / v_cache is NULL");
+        int rc = check_op_caches(c, k_cache, v_cache);
+        if (rc != TS_OK) return rc;
         if (num_seqs > 0 && (!block_table || !move_lens || !ctx_lens)) return fail(c, TS_ERR_INVALID_ARG, "block_table / move_lens / ctx_lens is NULL");
         int64_t total = 0;
         int last = -1;
@@ -1497,9 +1515,9 @@ extern "C" int ts_kv_move(ts_ctx* c, void* stream, void* k_cache, void* v_cache,
         if (!src || !dst) return fail(c, TS_ERR_INVALID_ARG, "src / dst is NULL");
         DeviceGuard guard(c->device);
         Op op{c, (hipStream_t)stream};
-        int rc = op.begin();
+        rc = op.begin();
         if (rc != TS_OK) return rc;
-        rc = check_op_pages(op, block_table, num_seqs, [&](int s) { return move_lens[s] > 0 ? (ctx_lens[s] + kPage - 1) / kPage : 0; });
+        rc = check_op_pages(op, block_table, num_seqs, [&](int s) { return move_lens[s] > 0 ? pages_up_to(ctx_lens[s]) : 0; });
         if (rc != TS_OK) return rc;
         MoveArgs a{};
         a.geo = geometry_of(c->desc);
@@ -1536,6 +1554,8 @@ extern "C" int ts_kv_read(ts_ctx* c, void* stream, const void* k_cache, const vo
         c->err.clear();
         if (num_seqs < 0) return fail(c, TS_ERR_INVALID_ARG, "num_seqs is negative");
         if (!k_cache || !v_cache) return fail(c, TS_ERR_INVALID_ARG, "k_cache / v_cache is NULL");
+        int rc = check_op_caches(c, k_cache, v_cache);
+        if (rc != TS_OK) return rc;
         if (c->desc.kv_dtype == TS_FP8_E4M3 && (!k_scale || !v_scale)) return fail(c, TS_ERR_INVALID_ARG, "fp8 cache needs k_scale and v_scale");
         if (num_seqs > 0 && (!block_table || !lens)) return fail(c, TS_ERR_INVALID_ARG, "block_table / lens is NULL");
         int64_t total = 0;
@@ -1552,9 +1572,9 @@ extern "C" int ts_kv_read(ts_ctx* c, void* stream, const void* k_cache, const vo
         if (!k_out && !v_out) return fail(c, TS_ERR_INVALID_ARG, "k_out and v_out are NULL");
         DeviceGuard guard(c->device);
         Op op{c, (hipStream_t)stream};
-        int rc = op.begin();
+        rc = op.begin();
         if (rc != TS_OK) return rc;
-        rc = check_op_pages(op, block_table, num_seqs, [&](int s) { return lens[s] > 0 ? (int32_t)(((starts ? (int64_t)starts[s] : 0) + lens[s] + kPage - 1) / kPage) : 0; });
+        rc = check_op_pages(op, block_table, num_seqs, [&](int s) { return lens[s] > 0 ? pages_up_to((starts ? (int64_t)starts[s] : 0) + lens[s]) : 0; });
         if (rc != TS_OK) return rc;
         ReadArgs a{};
         a.geo = geometry_of(c->desc);

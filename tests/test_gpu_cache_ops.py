@@ -727,3 +727,137 @@ def test_validated_page_table(bad):
     torch.cuda.synchronize()
     b.caches = [c.cpu().view(torch.bfloat16) for c in (kc, vc)]
     ctx.close()
+
+
+# ---- far pages, many rows, large trees, graphs that share the scratch, more refusals -------------------------------------
+
+@pytest.mark.parametrize("dtype,kind", KINDS)
+def test_pages_far_into_a_large_cache(dtype, kind):
+    """Pages behind the first 2^32 elements: the same bits as in a small cache."""
+    heads, base = (16, 8, 128), 262144 + 5
+    b = Batch(heads, dtype, kind, [5, 40, 1], [70, 300, 33], seed=90)
+    rng = np.random.default_rng(3)
+    masks = mask_on_gpu([tree_see(random_tree(rng, n)) for n in b.q_lens])
+    x = b.randn(b.T, 32, 128).cuda()
+    dev = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    src, dst, lens = dev([69, 68, 299, 5]), dev([65, 66, 261, 32]), [70, 300, 33]
+
+    def run(desc, kc, vc, table, ks, vs):
+        ctx = ts.Context(desc)
+        ctx.set_rope(64, layout="interleaved")
+        q, out = (torch.zeros((b.T, 16, 128), dtype=TORCH[dtype], device="cuda") for _ in range(2))
+        ko, vo = (torch.zeros((sum(lens), 8, 128), dtype=TORCH[dtype], device="cuda") for _ in range(2))
+        ctx.rope_kv_append(x[:, :16], x[:, 16:24], x[:, 24:], q, kc, vc, ks, vs, table, b.q_lens, b.ctx_lens)
+        ctx.tree_attention(q, kc, vc, ks, vs, table, masks, b.q_lens, b.ctx_lens, 0.0, out)
+        ctx.kv_move(kc, vc, table, src, dst, [2, 1, 1], b.ctx_lens)
+        ctx.kv_read(kc, vc, ks, vs, table, None, lens, ko, vo)
+        torch.cuda.synchronize()
+        ctx.close()
+        return [bits(t) for t in (q, out, ko, vo)]
+
+    kc, vc, ks, vs, table = b.on_gpu()
+    page = kc.numel() // b.pool
+    big = [torch.zeros((base + b.pool, page), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    for large, small in zip(big, (kc, vc)):
+        large[base:] = small.view(b.pool, page)
+    want = run(b.desc(), kc, vc, table, ks, vs)
+    got = run(ts.Desc.make(16, 8, 128, dtype, kind, base + b.pool, b.width), big[0].view(-1), big[1].view(-1), table + base, ks, vs)
+    for g, w in zip(got, want):
+        assert np.array_equal(g, w)
+    for large, small in zip(big, (kc, vc)):
+        assert torch.equal(large[base:].reshape(-1), small) and not large[:base].view(torch.int64).any()
+
+
+@pytest.mark.parametrize("dtype,kind", KINDS)
+@pytest.mark.parametrize("offset", [0, 1])
+def test_rope_append_decode_rows(dtype, kind, offset):
+    """Many single tokens, of which a workgroup takes several KV heads; in 16-byte pieces and element by element."""
+    rng = np.random.default_rng(11)
+    b = Batch((20, 5, 128), dtype, kind, np.ones(400, int), rng.integers(1, 60, 400), seed=91)
+    rope_case(b, dict(rot_dim=96, base=1e6), b.randn(b.T, 20, 128), b.randn(b.T, 5, 128), b.randn(b.T, 5, 128), strided=True, positions=None, offset=offset)
+
+
+@pytest.mark.parametrize("dtype,kind", KINDS)
+@pytest.mark.parametrize("shape", [([256], [256]), ([200, 3], [1800, 900]), ([64] * 12, [700] * 12), ([256] * 3, [300, 256, 257])])
+def test_tree_attention_large_trees(dtype, kind, shape):
+    """Trees of up to 256 nodes, with masks wider than needed, cut and whole, rows of a workgroup of every number."""
+    b = Batch((8, 2, 64), dtype, kind, *shape, seed=92)
+    rng = np.random.default_rng(12)
+    see = [tree_see(random_tree(rng, n, roots=3)) for n in b.q_lens]
+    see[0][[0, -1]] = False                                # (nothing but the prefix, if there is one)
+    q = b.randn(b.T, b.Hq, b.D)
+    got = tree_run(b, q, see, words=5)
+    check(got, *tree_reference(b, q, see))
+    if b.ctx_lens[0] == b.q_lens[0]:
+        assert (got[0] == 0).all() and (got[b.q_lens[0] - 1] == 0).all()
+
+
+def test_two_graphs_of_one_context():
+    """Two captured tree calls, whose scratch is the same, replayed in turn with an eager call between them."""
+    batches = [Batch((32, 8, 128), "bf16", "bf16", ql, cl, seed=93 + i) for i, (ql, cl) in enumerate((([12], [4000]), ([30, 7], [2500, 900])))]
+    width, pool = max(b.width for b in batches), max(b.pool for b in batches)
+    ctx, hip, stream = ts.Context(ts.Desc.make(32, 8, 128, "bf16", "bf16", pool, width)), _hip(), torch.cuda.Stream()
+    ctx.reserve_tree()
+    st, runs = ctypes.c_void_p(stream.cuda_stream), []
+    for b in batches:
+        see = [tree_see(random_tree(np.random.default_rng(1), n)) for n in b.q_lens]
+        kc, vc = (torch.zeros(pool * 8 * PAGE * 128, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        for c, x in zip((kc, vc), b.caches):
+            c[:x.numel()] = x.cuda()
+        table = np.full((len(b.q_lens), width), -1, np.int32)
+        table[:, :b.width] = b.table
+        q, mask, table = b.randn(b.T, 32, 128).cuda(), mask_on_gpu(see), torch.from_numpy(table).cuda()
+        outs = [torch.zeros_like(q) for _ in range(2)]
+        call = lambda out, s, b=b, q=q, kc=kc, vc=vc, table=table, mask=mask: ctx.tree_attention(  # noqa: E731
+            q, kc, vc, None, None, table, mask, b.q_lens, b.ctx_lens, 0.0, out, stream=s)
+        torch.cuda.synchronize()
+        graph, execg = ctypes.c_void_p(), ctypes.c_void_p()
+        assert hip.hipStreamBeginCapture(st, 2) == 0
+        call(outs[0], stream)
+        assert hip.hipStreamEndCapture(st, ctypes.byref(graph)) == 0
+        assert hip.hipGraphInstantiate(ctypes.byref(execg), graph, None, None, ctypes.c_size_t(0)) == 0
+        runs.append((call, outs, q, graph, execg))
+    for i in range(3):
+        for call, outs, q, graph, execg in runs:
+            q.normal_()
+            outs[0].fill_(float("nan"))
+        torch.cuda.synchronize()
+        for call, outs, q, graph, execg in runs:
+            assert hip.hipGraphLaunch(execg, st) == 0
+        torch.cuda.synchronize()
+        for call, outs, q, graph, execg in runs:
+            call(outs[1], None)
+        torch.cuda.synchronize()
+        for call, outs, q, graph, execg in runs:
+            assert np.array_equal(bits(outs[0]), bits(outs[1])), i
+    for call, outs, q, graph, execg in runs:
+        assert hip.hipGraphExecDestroy(execg) == 0 and hip.hipGraphDestroy(graph) == 0
+    ctx.close()
+
+
+def test_refusals_of_addresses_and_rows():
+    """Rows that overlap (an expanded tensor's stride of 0 is not that of packed rows); caches and masks off their alignment."""
+    b = Batch((8, 2, 64), "bf16", "bf16", [3, 2], [20, 40], seed=94)
+    ctx, lib = ts.Context(b.desc()), ts.load_library()
+    ctx.set_rope(64)
+    kc, vc, ks, vs, table = b.on_gpu()
+    q, k, v = (b.randn(b.T, h, 64).cuda() for h in (8, 2, 2))
+    out, mask, i5 = torch.full_like(q, 7.0), torch.zeros((b.T + 1, 1), dtype=torch.int64, device="cuda"), torch.zeros(5, dtype=torch.int32, device="cuda")
+    before = [t.clone() for t in (kc, vc)]
+    for i in range(3):
+        rows = [q, k, v]
+        rows[i] = rows[i][:1].expand(b.T, -1, -1)
+        with pytest.raises(ValueError):
+            ctx.rope_kv_append(*rows, out, kc, vc, ks, vs, table, b.q_lens, b.ctx_lens)
+    lens = lambda *a: np.asarray(a, np.int32).tobytes()  # noqa: E731
+    ql, cl, t = lens(*b.q_lens), lens(*b.ctx_lens), table.data_ptr()
+    for dk, dv in ((8, 0), (0, 4)):
+        kp, vp = kc.data_ptr() + dk, vc.data_ptr() + dv
+        assert lib.ts_rope_kv_append(ctx._h, 0, q.data_ptr(), 0, k.data_ptr(), 0, v.data_ptr(), 0, out.data_ptr(), kp, vp, 0, 0, t, 0, ql, cl, 2) == binding.TS_ERR_INVALID_ARG
+        assert lib.ts_tree_attention(ctx._h, 0, q.data_ptr(), kp, vp, 0, 0, t, mask.data_ptr(), 1, ql, cl, 2, 0.0, out.data_ptr()) == binding.TS_ERR_INVALID_ARG
+        assert lib.ts_kv_move(ctx._h, 0, kp, vp, t, i5.data_ptr(), i5.data_ptr(), ql, cl, 2) == binding.TS_ERR_INVALID_ARG
+        assert lib.ts_kv_read(ctx._h, 0, kp, vp, 0, 0, t, None, ql, 2, out.data_ptr(), None) == binding.TS_ERR_INVALID_ARG
+    assert lib.ts_tree_attention(ctx._h, 0, q.data_ptr(), kc.data_ptr(), vc.data_ptr(), 0, 0, t, mask.data_ptr() + 4, 1, ql, cl, 2, 0.0, out.data_ptr()) == binding.TS_ERR_INVALID_ARG
+    torch.cuda.synchronize()
+    assert (out == 7.0).all() and torch.equal(kc, before[0]) and torch.equal(vc, before[1])
+    ctx.close()
