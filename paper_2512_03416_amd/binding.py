@@ -197,16 +197,19 @@ def _i32_bytes(a) -> bytes:
     return np.asarray(a, dtype=np.int32).tobytes()
 
 
-def _host_lens(first, *others):
-    """([int32 arrays as bytes], their common length, the sum of the first one)."""
-    arrays = [np.asarray(a, dtype=np.int32) for a in (first, *others)]
-    n = arrays[0].size
-    for a in arrays:
-        if a.size != n:
-            raise ValueError(f"lengths of {[x.size for x in arrays]} sequences")
+def _host_lens(first, second=None):
+    """(first, second: int32 arrays as bytes, second may be None; their common length; the sum of the first)."""
+    one = np.asarray(first, dtype=np.int32)
+    n = one.size
+    other = None
+    if second is not None:
+        two = np.asarray(second, dtype=np.int32)
+        if two.size != n:
+            raise ValueError(f"lengths of {[n, two.size]} sequences")
+        other = two.tobytes()
     # (adding up a short list takes a tenth of numpy's sum)
-    total = sum(arrays[0].reshape(-1).tolist()) if n < 64 else int(arrays[0].sum(dtype=np.int64))
-    return [a.tobytes() for a in arrays], n, total
+    total = sum(one.reshape(-1).tolist()) if n < 64 else int(one.sum(dtype=np.int64))
+    return one.tobytes(), other, n, total
 
 
 def _count(lens) -> int:
@@ -403,9 +406,12 @@ class Context:
         """(device pointer, elements from row to row) of token rows [tokens, heads, dim], whose heads and dims are packed."""
         if t is None:
             return 0, 0
-        dim, shape = self._dim, t.shape
-        if len(shape) != 3 or shape[1] != heads or shape[2] != dim or shape[0] < total:
-            raise ValueError(f"{name} has shape {tuple(shape)}, expected [{total}, {heads}, {dim}]")
+        dim = self._dim
+        if t.dim() != 3:
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected [{total}, {heads}, {dim}]")
+        tokens, h, d = t.shape
+        if tokens < total or h != heads or d != dim:
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected [{total}, {heads}, {dim}]")
         if total == 0:
             return 0, 0
         if t.get_device() != self.device:
@@ -433,17 +439,25 @@ class Context:
             raise ValueError(f"{name} must be contiguous")
         return t.data_ptr()
 
+    def _cache_ptrs(self, k_cache, v_cache, k_scale, v_scale):
+        """Device pointers of the caches and their scales."""
+        ks = 0 if k_scale is None else self._ptr(k_scale, "k_scale", self._f32, self._hkv)
+        vs = 0 if v_scale is None else self._ptr(v_scale, "v_scale", self._f32, self._hkv)
+        return self._cache_ptr(k_cache, "k_cache"), self._cache_ptr(v_cache, "v_cache"), ks, vs
+
     def rope_kv_append(self, q, k_new, v_new, q_out, k_cache, v_cache, k_scale, v_scale, block_table, q_lens, ctx_lens,
                        positions=None, stream=None):
         """q, k_new, v_new: [T, heads, dim], rows may be strided (slices of one projection's output); q_out packed, may be q."""
         ptr, rows, hq, hkv = self._ptr, self._rows, self._hq, self._hkv
-        (ql, cl), n, total = _host_lens(q_lens, ctx_lens)
-        rc = self._lib.ts_rope_kv_append(self._h, self._stream(stream, self.device), *rows(q, "q", hq, total), *rows(k_new, "k_new", hkv, total),
-                                         *rows(v_new, "v_new", hkv, total), ptr(q_out, "q_out", self._q_type, total * hq * self._dim),
-                                         self._cache_ptr(k_cache, "k_cache"), self._cache_ptr(v_cache, "v_cache"),
-                                         ptr(k_scale, "k_scale", self._f32, hkv), ptr(v_scale, "v_scale", self._f32, hkv),
+        ql, cl, n, total = _host_lens(q_lens, ctx_lens)
+        q_at, q_row = rows(q, "q", hq, total)
+        k_at, k_row = rows(k_new, "k_new", hkv, total)
+        v_at, v_row = rows(v_new, "v_new", hkv, total)
+        kc, vc, ks, vs = self._cache_ptrs(k_cache, v_cache, k_scale, v_scale)
+        rc = self._lib.ts_rope_kv_append(self._h, self._stream(stream, self.device), q_at, q_row, k_at, k_row, v_at, v_row,
+                                         ptr(q_out, "q_out", self._q_type, total * hq * self._dim), kc, vc, ks, vs,
                                          ptr(block_table, "block_table", self._i32, n * self._width),
-                                         ptr(positions, "positions", self._i32, total), ql, cl, n)
+                                         0 if positions is None else ptr(positions, "positions", self._i32, total), ql, cl, n)
         if rc != TS_OK:
             self._check(rc)
 
@@ -455,16 +469,15 @@ class Context:
                        stream=None):
         """tree_mask: int64 [T, words] on the GPU (see tree_masks), or None for chains."""
         ptr = self._ptr
-        (ql, cl), n, total = _host_lens(q_lens, ctx_lens)
+        ql, cl, n, total = _host_lens(q_lens, ctx_lens)
         words = 0
         if tree_mask is not None:
             if tree_mask.dim() != 2:
                 raise ValueError(f"tree_mask has shape {tuple(tree_mask.shape)}, expected [tokens, words]")
             words = tree_mask.shape[1]
         elems = total * self._hq * self._dim
-        rc = self._lib.ts_tree_attention(self._h, self._stream(stream, self.device), ptr(q, "q", self._q_type, elems), self._cache_ptr(k_cache, "k_cache"),
-                                         self._cache_ptr(v_cache, "v_cache"), ptr(k_scale, "k_scale", self._f32, self._hkv),
-                                         ptr(v_scale, "v_scale", self._f32, self._hkv),
+        kc, vc, ks, vs = self._cache_ptrs(k_cache, v_cache, k_scale, v_scale)
+        rc = self._lib.ts_tree_attention(self._h, self._stream(stream, self.device), ptr(q, "q", self._q_type, elems), kc, vc, ks, vs,
                                          ptr(block_table, "block_table", self._i32, n * self._width),
                                          ptr(tree_mask, "tree_mask", self._i64, total * words), words, ql, cl, n, sm_scale,
                                          ptr(out, "out", self._q_type, elems))
@@ -474,8 +487,9 @@ class Context:
     def kv_move(self, k_cache, v_cache, block_table, src, dst, move_lens, ctx_lens, stream=None):
         """Entries at positions dst take what positions src held; pairs packed by sequence, -1 = no pair."""
         ptr = self._ptr
-        (ml, cl), n, total = _host_lens(move_lens, ctx_lens)
-        rc = self._lib.ts_kv_move(self._h, self._stream(stream, self.device), self._cache_ptr(k_cache, "k_cache"), self._cache_ptr(v_cache, "v_cache"),
+        ml, cl, n, total = _host_lens(move_lens, ctx_lens)
+        kc, vc, _, _ = self._cache_ptrs(k_cache, v_cache, None, None)
+        rc = self._lib.ts_kv_move(self._h, self._stream(stream, self.device), kc, vc,
                                   ptr(block_table, "block_table", self._i32, n * self._width),
                                   ptr(src, "src", self._i32, total), ptr(dst, "dst", self._i32, total), ml, cl, n)
         if rc != TS_OK:
@@ -484,14 +498,10 @@ class Context:
     def kv_read(self, k_cache, v_cache, k_scale, v_scale, block_table, starts, lens, k_out, v_out, stream=None):
         """Tokens starts .. starts + lens - 1 of every sequence as rows [sum of lens, KV heads, dim]; starts None = 0."""
         ptr = self._ptr
-        if starts is None:
-            (ln,), n, total = _host_lens(lens)
-            st = None
-        else:
-            (ln, st), n, total = _host_lens(lens, starts)
+        ln, st, n, total = _host_lens(lens, starts)
         elems = total * self._hkv * self._dim
-        rc = self._lib.ts_kv_read(self._h, self._stream(stream, self.device), self._cache_ptr(k_cache, "k_cache"), self._cache_ptr(v_cache, "v_cache"),
-                                  ptr(k_scale, "k_scale", self._f32, self._hkv), ptr(v_scale, "v_scale", self._f32, self._hkv),
+        kc, vc, ks, vs = self._cache_ptrs(k_cache, v_cache, k_scale, v_scale)
+        rc = self._lib.ts_kv_read(self._h, self._stream(stream, self.device), kc, vc, ks, vs,
                                   ptr(block_table, "block_table", self._i32, n * self._width), st, ln, n,
                                   ptr(k_out, "k_out", self._q_type, elems), ptr(v_out, "v_out", self._q_type, elems))
         if rc != TS_OK:
