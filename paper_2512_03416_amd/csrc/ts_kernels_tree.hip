@@ -2,8 +2,8 @@
 //
 // Every node of a tree sees the sequence's prefix and its own ancestors, so all nodes of a sequence share the scan of the
 // prefix: row (node, head of the group) is a column of S^T = K Q^T, and a workgroup reads K and V once for all its rows.
-//   - Four waves of 32 columns: WR of them side by side over the rows, WK = 4 / WR of them taking turns along the keys.  Up to 32
-//     rows: WR = 1, each wave scans its own keys.
+//   - Four waves of 32 columns: WR of them side by side over the rows, WK = 4 / WR of them taking turns along the keys.  A workgroup
+//     has 32 WR rows; with WR = 1 each wave scans keys of its own.
 //   - Keys come in steps of 32 (two pages) per wave, copied into a ring of LDS slots by the memory system, in the order in which
 //     the matrix instructions take them: a wave's operand read is always 1 KB in lane order (no bank conflicts), and copies in
 //     flight take no registers.  The WR waves of a key group share the copy.
@@ -26,22 +26,25 @@ constexpr float kBigTr = 65536.0f;
 // Reference maximum of a column that has seen no key: finite, so that differences stay defined.
 constexpr float kNoKeyTr = -3.402823466e38f;
 
-// LDS image of 32 keys (two pages), in blocks of 64 pieces of 16 bytes:
-//   K block j: piece (h, n) = 16-byte chunk 2j + h of token swap23(n % 16) of page n / 16
-//   V, bf16: block (page p, dims 32 d ..): piece (h, n) = tokens 8h .. 8h + 7 of dim 32 d + n;  e4m3: block d: piece (p, n) = the
-//   16 tokens of dim 32 d + n of page p;  fp32: block (p, d, i): piece (h, n) = tokens 8h + 4i .. + 3
+// LDS image of 32 keys (two pages), in blocks of 64 pieces of 16 bytes, each of one page, so that a copy takes a scalar base and a lane's
+// offset that never changes (with bases per lane, 32 trees of 64 nodes over 8 Ki tokens took 600 us instead of 566):
+//   K block i of a page: piece 16 c + t = 16-byte chunk 4i + c of token swap23(t)
+//   V, bf16: block d: piece (h, n) = tokens 8h .. 8h + 7 of dim 32 d + n;  e4m3: block i: piece n = the 16 tokens of dim 64 i + n;
+//   fp32: block (d, i): piece (h, n) = tokens 8h + 4i .. + 3 of dim 32 d + n
 template <typename KT, int D> struct TrStep {
     static constexpr int ES = (int)sizeof(KT), PB = 16 * D * ES;       // bytes of an element, of a tile
-    static constexpr int NK = D * ES / 32, NV = NK, NB = NK + NV;      // blocks
+    static constexpr int NK = D * ES / 32, NV = NK, NB = NK + NV;      // blocks of K, of V, of both
+    static constexpr int HK = NK / 2;                                  // blocks of a page's K (or V)
     static constexpr int kBytes = NB * 1024;
 };
 __device__ __forceinline__ int tr_swap23(int s) { return (s & 3) | ((s & 4) << 1) | ((s & 8) >> 1); }
 
 __device__ __forceinline__ uint32_t tr_lds_address(const void* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p; }
-// 64 x 16 bytes straight into LDS, lane l's at lds + 16 l; counted by vmcnt.
-__device__ __forceinline__ void tr_copy(uint32_t lds, const char* p)
+// 64 x 16 bytes straight into LDS, lane l's from base + offset to lds + 16 l; counted by vmcnt.  (The wait states: m0 is read one
+// instruction after it was written at the earliest, a scalar register that a vector instruction wrote -- a spilled one read back -- five.)
+__device__ __forceinline__ void tr_copy(uint32_t lds, const char* base, uint32_t offset)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n" :: "s"(lds), "v"(p) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2\n" :: "s"(lds), "v"(offset), "s"(base) : "memory", "m0");
 }
 template <int N> __device__ __forceinline__ void tr_wait_copies()
 {
@@ -49,29 +52,29 @@ template <int N> __device__ __forceinline__ void tr_wait_copies()
     __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4 << 14));    // vmcnt(N); expcnt and lgkmcnt untouched
 }
 
+// Where a lane's pieces lie in the first block of a page's K and V.
+struct TrOffsets { uint32_t k, v; };
+template <typename KT, int D>
+__device__ __forceinline__ TrOffsets tr_offsets(int lane)
+{
+    constexpr int ES = (int)sizeof(KT);
+    const int n = lane & 31, h = lane >> 5;
+    return TrOffsets{(uint32_t)((lane >> 4) * 256 + tr_swap23(lane & 15) * 16), (uint32_t)(ES == 1 ? lane * 16 : n * (16 * ES) + h * (8 * ES))};
+}
 // The blocks wr, wr + WR, ... of two pages on their way into LDS.
 template <int WR, typename KT, int D>
-__device__ __forceinline__ void tr_copy_step(uint32_t lds, const char* kc, const char* vc, int64_t tile0, int64_t tile1, int wr, int lane)
+__device__ __forceinline__ void tr_copy_step(uint32_t lds, const char* k0, const char* k1, const char* v0, const char* v1, int wr, TrOffsets at)
 {
     using S = TrStep<KT, D>;
-    const int n = lane & 31, h = lane >> 5;
-    const char* k = kc + (n >= 16 ? tile1 : tile0) * S::PB + h * 256 + tr_swap23(n & 15) * 16;
 #pragma unroll
     for (int i = 0; i < S::NB / WR; ++i) {
         const int b = wr + WR * i;
-        const char* p;
-        if (b < S::NK) p = k + b * 512;
-        else {
-            const int v = b - S::NK;
-            if constexpr (S::ES == 1) p = vc + (h ? tile1 : tile0) * S::PB + (32 * v + n) * 16;
-            else {
-                constexpr int PER = S::NV / 2;                         // blocks of a page
-                const int in = v % PER;
-                const int d = S::ES == 2 ? in : in / 2, i16 = S::ES == 2 ? 0 : in % 2;
-                p = vc + (v >= PER ? tile1 : tile0) * S::PB + (32 * d + n) * (16 * S::ES) + h * (8 * S::ES) + i16 * 16;
-            }
-        }
-        tr_copy(lds + b * 1024, p);
+        const bool is_v = S::NK % WR == 0 ? i >= S::NK / WR : b >= S::NK;
+        const int c = is_v ? b - S::NK : b;
+        const bool second = S::HK % WR == 0 ? i % (S::NK / WR) >= S::HK / WR : c >= S::HK;
+        const int block = second ? c - S::HK : c;
+        const int from = S::ES == 4 && is_v ? (block >> 1) * 2048 + (block & 1) * 16 : block * 1024;
+        tr_copy(lds + b * 1024, (is_v ? (second ? v1 : v0) : (second ? k1 : k0)) + from, is_v ? at.v : at.k);
     }
 }
 
@@ -109,12 +112,18 @@ template <typename KT, int D> struct TrK {
     static constexpr int N = sizeof(KT) == 4 ? 1 : TrStep<KT, D>::NK;
     uint4 piece[N];
 };
+// Lane (h, n)'s chunk h of token swap23(n % 16) of page n / 16; its chunks 2b + h lie 512 bytes apart.
+template <typename KT, int D>
+__device__ __forceinline__ int tr_k_at(int lane)
+{
+    return (lane >> 4 & 1) * (TrStep<KT, D>::HK * 1024) + (lane >> 5) * 256 + (lane & 15) * 16;
+}
 template <typename KT, int D>
 __device__ __forceinline__ void tr_load_k(TrK<KT, D>& k, const unsigned char* lk, int lane)
 {
     if constexpr (sizeof(KT) != 4) {
 #pragma unroll
-        for (int b = 0; b < TrK<KT, D>::N; ++b) k.piece[b] = *(const uint4*)(lk + b * 1024 + lane * 16);
+        for (int b = 0; b < TrK<KT, D>::N; ++b) k.piece[b] = *(const uint4*)(lk + tr_k_at<KT, D>(lane) + b * 512);
     }
 }
 template <typename KT, int D>
@@ -124,7 +133,7 @@ __device__ __forceinline__ f32x16 tr_scores(const TrK<KT, D>& k, [[maybe_unused]
     if constexpr (sizeof(KT) == 4) {
 #pragma unroll
         for (int b = 0; b < TrStep<KT, D>::NK; ++b) {
-            const f32x4 kf = *(const f32x4*)(lk + b * 1024 + lane * 16);
+            const f32x4 kf = *(const f32x4*)(lk + tr_k_at<KT, D>(lane) + b * 512);
 #pragma unroll
             for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], q.q[b][e], s, 0, 0, 0);
         }
@@ -150,7 +159,7 @@ __device__ __forceinline__ TrV<KT, D> tr_load_v(const unsigned char* lv, int p, 
     TrV<KT, D> v;
     constexpr int DB = D / 32;
     if constexpr (sizeof(KT) == 1) {
-        const uint2 x = *(const uint2*)(lv + d * 1024 + (p * 32 + (lane & 31)) * 16 + (lane >> 5) * 8);
+        const uint2 x = *(const uint2*)(lv + (p * TrStep<KT, D>::HK + (d >> 1)) * 1024 + ((d & 1) * 32 + (lane & 31)) * 16 + (lane >> 5) * 8);
         v.w[0] = x.x; v.w[1] = x.y;
     } else {
         constexpr int I = (int)sizeof(KT) / 2;
@@ -188,8 +197,8 @@ __device__ __forceinline__ bool tr_clean_v(TrV<KT, D>& v, int have)
 
 __device__ __forceinline__ uint32_t pack_bf16(float x, float y) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, bf16x2)); }
 
-// The keys from node number j0 on (j0 a multiple of 8 below node 0 or anything; negative: the prefix, which everybody sees) that
-// a node sees, as bits 0 .. 7; nodes from n_nodes on do not exist.  Without a mask a node sees those up to itself.
+// Which of the eight keys from node number j0 on a node sees, as bits 0 .. 7.  Negative numbers are the prefix, which everybody sees;
+// nodes from n_nodes on do not exist.  Without a mask a node sees those up to itself.
 // There is no divergent branch here or anywhere else in the steps: the compiler was seen to save a register before the lanes of such
 // a branch are back together, so that the others' values (addresses of the next copies) were lost.
 __device__ __forceinline__ uint32_t tr_visible(const uint64_t* mask, int words, int n_nodes, int node, int j0)
@@ -280,17 +289,19 @@ __global__ __launch_bounds__(64 * kTrWaves) void tree_kernel(TreeArgs a, TreeSeq
     const bool works = first_row < it.node_rows;               // (a wave without rows only copies)
 
     const int32_t TS_CONSTANT* bt = as_constant(a.block_table) + (int64_t)it.seq * a.geo.max_pages;
-    const char* kc = (const char*)a.k_cache;
-    const char* vc = (const char*)a.v_cache;
+    const char* kc = (const char*)a.k_cache + (int64_t)it.g * S::PB;
+    const char* vc = (const char*)a.v_cache + (int64_t)it.g * S::PB;
+    const uint32_t page_bytes = (uint32_t)Hkv * S::PB;         // of all heads: below 2^32 (checked by the call)
+    const TrOffsets at = tr_offsets<KT, D>(lane);
     // (past the end of the range: its last page again, whose keys do not count a second time)
     auto page_of = [&](int i) { return page0 + 2 * (WK * i + kg); };
     auto id_of = [&](int page) { return bt[min(page, page1 - 1)]; };
     // (page ids are asked for a step ahead; the opaque copies keep the wait for them where they are used)
     int32_t next0 = id_of(page_of(0)), next1 = id_of(page_of(0) + 1);
     auto issue = [&](int i) {
-        const int64_t tile0 = (int64_t)opaque_uniform(next0) * Hkv + it.g, tile1 = (int64_t)opaque_uniform(next1) * Hkv + it.g;
+        const uint64_t p0 = (uint64_t)(uint32_t)opaque_uniform(next0) * page_bytes, p1 = (uint64_t)(uint32_t)opaque_uniform(next1) * page_bytes;
         next0 = id_of(page_of(i + 1)); next1 = id_of(page_of(i + 1) + 1);
-        tr_copy_step<WR, KT, D>(tr_lds_address(ring[i % R][kg]), kc, vc, tile0, tile1, wr, lane);
+        tr_copy_step<WR, KT, D>(tr_lds_address(ring[i % R][kg]), kc + p0, kc + p1, vc + p0, vc + p1, wr, at);
     };
     // the copies of a step have landed, those of up to `later` steps behind it may be under way; then everybody's have
     auto wait = [&](int later) {

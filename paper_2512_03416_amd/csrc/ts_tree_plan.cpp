@@ -88,6 +88,8 @@ struct TreeTimes {
     double page_full;                  // the same with a workgroup in every place: bound by the matrix products, the softmax and the LDS
     double page_read;                  // a page read from HBM, by whichever of its groups of rows comes first
     int64_t places;                    // workgroups resident at once
+    double item;                       // a workgroup's fixed share of its CU: 29 trees of 16 nodes over 10 tokens (64/8 heads) take 10.7 us in 232
+                                       // workgroups of 128 rows, 14.9 in 464 of 64, 28 in 928 of 32
     double start, round;               // launch, page ids, queries, first copies, last stores; of a later workgroup in the same place
     double merge, merge_row;           // merge launch, and a partial row written and read again
 };
@@ -105,11 +107,12 @@ static TreeTimes tree_times(const ts_attn_desc& d, int rows, int n_cu)
     const int per_cu = std::max(1, std::min(2, 160 * 1024 / (slot * tree_ring_slots(slot))));
     t.places = (int64_t)n_cu * per_cu;
     t.page_alone = 0.36 * rows / 128 * (0.3 + 0.7 * dims) * math;
-    // 32 trees of 64 nodes over 8 Ki tokens (64/8 heads of 128): bf16 594 us with 128 rows, 639 with 64, 971 with 32 (one workgroup per CU, and
-    // L2 reads of 17 TB/s); 8 trees of 100-128 nodes over 2-9 Ki, e4m3: 219, 191, 203
+    // 32 trees of 64 nodes over 8 Ki tokens (64/8 heads of 128): bf16 558 us with 128 rows, 630 with 64, 1016 with 32 (one workgroup per CU, and
+    // L2 reads of 17 TB/s), e4m3 530, 564, 628; 8 trees of 100-128 nodes over 2-9 Ki, e4m3: 208, 187, 199
     const bool e4m3 = elem == 1;
-    t.page_full = (rows == 32 ? (per_cu == 1 ? 0.118 : (e4m3 ? 0.155 : 0.16)) : (rows == 64 ? (per_cu == 1 ? 0.2 : (e4m3 ? 0.28 : 0.31)) : (per_cu == 1 ? 0.36 : (e4m3 ? 0.57 : 0.55)))) * dims * math;
+    t.page_full = (rows == 32 ? (per_cu == 1 ? 0.118 : (e4m3 ? 0.155 : 0.16)) : (rows == 64 ? (per_cu == 1 ? 0.2 : (e4m3 ? 0.288 : 0.335)) : (per_cu == 1 ? 0.36 : (e4m3 ? 0.54 : 0.52)))) * dims * math;
     t.page_read = 2.0 * kPage * d.head_dim * elem / 6.2e6;     // 6.2 TB/s
+    t.item = 4.0;
     t.start = 5.0;
     t.round = 2.5;
     t.merge = 6.0;
@@ -118,18 +121,20 @@ static TreeTimes tree_times(const ts_attn_desc& d, int rows, int n_cu)
 }
 
 // Rows per workgroup: 128 share every copied page four ways; with 32, each wave copies and scans keys of its own and waits for no other,
-// which is faster wherever L2 and HBM keep up (4 trees of 7-26 nodes over 0.5-2.5 Ki tokens, 32/8 heads, 17.0 us with 32 rows, 19.6 with 128).
+// which is faster wherever L2 and HBM keep up (4 trees of 7-26 nodes over 0.5-2.5 Ki tokens, 32/8 heads, 16.9 us with 32 rows, 19.5 with 128).
 // Cuts: uncut, a scan writes no partial results, and the longest scans come first, so that a batch with a workgroup or more for every place
-// comes out even by itself: 32 trees of 32-64 nodes over 1-8 Ki tokens (64/8 heads) take 284 us uncut, 297 in ranges of at most 384
-// pages, 317 in ranges of 192.  Smaller batches are cut until the workgroups fill the places: 8 trees of 30 nodes over 4000 tokens
-// (32/8 heads, 128 rows) 92 us uncut, 38 in ranges of 32 to 64 pages, 54 in ranges of 16 (most of it partial results).  Ranges of a sequence
-// are of one length.  Both are taken from the times above, which come within a tenth of the best choice on these batches and eight more.
+// comes out even by itself: 32 trees of 32-64 nodes over 1-8 Ki tokens (64/8 heads) take 287 us uncut, 312 in ranges of at most 384
+// pages, 325 in ranges of 192.  Smaller batches are cut until the workgroups fill the places: 8 trees of 30 nodes over 4000 tokens
+// (32/8 heads, 128 rows) 92 us uncut, 39 to 41 in ranges of 32 to 64 pages, 53 in ranges of 16 (most of it partial results).  Ranges of a sequence
+// are of one length.  Both are taken from the times above, which come within 6 % of the best number of rows on these batches and 20 more.
 void plan_tree(const ts_attn_desc& d, const int32_t* q_lens, const int32_t* ctx_lens, int num_seqs, int n_cu, TreePlan* plan)
 {
     const int32_t G = d.num_q_heads / d.num_kv_heads, Hkv = d.num_kv_heads;
     plan->seqs.clear();
-    int64_t most = 0, row = 0, scans = 0;                      // most rows of a sequence; pages of all scans
+    int64_t most = 0, row = 0;                                 // most rows of a sequence
     int32_t longest = 0;
+    const double page_bytes = 2.0 * kPage * d.head_dim * (d.kv_dtype == TS_F32 ? 4 : (d.kv_dtype == TS_BF16 ? 2 : 1));
+    double held = 0.0;                                         // bytes of all scans
     auto pages_of = [](const TreeSeq& s) { return (s.prefix + s.n_nodes + kPage - 1) / kPage; };
     for (int s = 0; s < num_seqs; ++s) {
         if (q_lens[s] > 0) {
@@ -137,7 +142,7 @@ void plan_tree(const ts_attn_desc& d, const int32_t* q_lens, const int32_t* ctx_
             plan->seqs.push_back(TreeSeq{s, (int32_t)row, q_lens[s], ctx_lens[s] - q_lens[s], 0, 1, 0, 0, 0});
             const int32_t pages = pages_of(plan->seqs.back());
             longest = std::max(longest, pages);
-            scans += pages;
+            held += (double)pages * Hkv * page_bytes;
         }
         row += q_lens[s];
     }
@@ -153,6 +158,9 @@ void plan_tree(const ts_attn_desc& d, const int32_t* q_lens, const int32_t* ctx_
             }
         }
     };
+    // What a group reads after another one comes from HBM again now and then, unless the batch fits the 256 MB behind the L2 caches
+    // (14 trees of 9-25 nodes over 2-27 Ki tokens, 32/8 heads: 188 us with 32 rows, 160 with 128).
+    const double again = held > 256e6 ? 0.15 : 0.05;
     std::vector<std::pair<int32_t, int32_t>> ranges;
     plan->rows = 128;
     int32_t best = 0;
@@ -164,7 +172,11 @@ void plan_tree(const ts_attn_desc& d, const int32_t* q_lens, const int32_t* ctx_
         const int32_t round = tree_round(rows_wg), whole = (longest + round - 1) / round * round;
         auto groups_of = [&](const TreeSeq& s) { return tree_groups(s.n_nodes, G, rows_wg); };
         int64_t total = 0;                                     // pages of all scans' groups of rows
-        for (const TreeSeq& s : plan->seqs) total += (int64_t)pages_of(s) * groups_of(s);
+        double reads = 0.0;                                    // ... that come from HBM
+        for (const TreeSeq& s : plan->seqs) {
+            total += (int64_t)pages_of(s) * groups_of(s);
+            reads += pages_of(s) * (1.0 + again * (groups_of(s) - 1));
+        }
         for (int32_t L = whole; L >= round; L = std::min((L / 4 * 3 + round - 1) / round * round, L - round)) {
             int64_t items = 0, rows = 0;
             int32_t len = 0;
@@ -189,7 +201,7 @@ void plan_tree(const ts_attn_desc& d, const int32_t* q_lens, const int32_t* ctx_
                 time = std::max(time, 0.85 * (len * t.page_alone + ranges[k].first * std::max(0.0, t.page_full - t.page_alone)));
             }
             if (items > t.places) time += 0.15 * page * total * Hkv / items + ((double)items / t.places - 1.0) * t.round;
-            time = t.start + std::max(time, scans * Hkv * t.page_read);
+            time = t.start + std::max({time, reads * Hkv * t.page_read, (double)items / n_cu * t.item});
             if (rows > 0) time += t.merge + rows * t.merge_row;
             if (best == 0 || time < best_time) { plan->rows = rows_wg; best = L; best_time = time; }
             if (items > 4 * t.places) break;
