@@ -383,10 +383,14 @@ struct TreePlan {
 };
 void plan_tree(const ts_attn_desc& d, const int32_t* q_lens, const int32_t* ctx_lens, int num_seqs, int n_cu, TreePlan* plan);
 inline int32_t tree_groups(int32_t nodes, int32_t G, int32_t rows) { return (int32_t)(((int64_t)nodes * G + rows - 1) / rows); }
-// LDS that a workgroup of the tree kernel takes: a ring of up to four slots of 32 keys for each of its 4 * 32 / rows groups of waves, in
-// at most 80 of the 160 KB of a CU, but at least two slots.
+// LDS that a workgroup of the tree kernel takes: a ring of up to four slots of 32 keys (five of bf16, whose steps overlap) for each of its
+// 4 * 32 / rows groups of waves, in at most 80 of the 160 KB of a CU, but at least two slots.
 constexpr int kTreeWaves = 4;
-constexpr int tree_ring_slots(int slot_bytes) { return 80 * 1024 / slot_bytes < 2 ? 2 : (80 * 1024 / slot_bytes > 4 ? 4 : 80 * 1024 / slot_bytes); }
+constexpr int tree_ring_slots(int slot_bytes, bool bf16)
+{
+    const int fit = 80 * 1024 / slot_bytes, most = bf16 ? 5 : 4;
+    return fit < 2 ? 2 : (fit > most ? most : fit);
+}
 
 // Heads that one workgroup of the rotary append takes of a page's tokens (RopeArgs).
 void rope_slices(const ts_attn_desc& d, int64_t tokens, int64_t units, int n_cu, bool with_q, RopeArgs* a);

@@ -27,7 +27,8 @@ constexpr float kBigTr = 65536.0f;
 constexpr float kNoKeyTr = -3.402823466e38f;
 
 // LDS image of 32 keys (two pages), in blocks of 64 pieces of 16 bytes, each of one page, so that a copy takes a scalar base and a lane's
-// offset that never changes (with bases per lane, 32 trees of 64 nodes over 8 Ki tokens took 600 us instead of 566):
+// offset that never changes (with bases per lane, 32 trees of 64 nodes over 8 Ki tokens took 600 us instead of 566, with steps
+// one after the other):
 //   K block i of a page: piece 16 c + t = 16-byte chunk 4i + c of token swap23(t)
 //   V, bf16: block d: piece (h, n) = tokens 8h .. 8h + 7 of dim 32 d + n;  e4m3: block i: piece n = the 16 tokens of dim 64 i + n;
 //   fp32: block (d, i): piece (h, n) = tokens 8h + 4i .. + 3 of dim 32 d + n
@@ -50,6 +51,15 @@ template <int N> __device__ __forceinline__ void tr_wait_copies()
 {
     static_assert(N >= 0 && N < 64, "vmcnt");
     __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4 << 14));    // vmcnt(N); expcnt and lgkmcnt untouched
+}
+
+// At most `later` steps of C copies each, N at the most, are under way behind this.
+template <int N, int C>
+__device__ __forceinline__ void tr_wait_steps(int later)
+{
+    if constexpr (N == 0) tr_wait_copies<0>();
+    else if (later >= N) tr_wait_copies<N * C>();
+    else tr_wait_steps<N - 1, C>(later);
 }
 
 // Where a lane's pieces lie in the first block of a page's K and V.
@@ -126,6 +136,17 @@ __device__ __forceinline__ void tr_load_k(TrK<KT, D>& k, const unsigned char* lk
         for (int b = 0; b < TrK<KT, D>::N; ++b) k.piece[b] = *(const uint4*)(lk + tr_k_at<KT, D>(lane) + b * 512);
     }
 }
+// The A operand of 16 dims (the b-th of Q^T's): a piece, or half of an e4m3 one, widened.
+template <typename KT, int D>
+__device__ __forceinline__ bf16x8 tr_k_operand(const TrK<KT, D>& k, int b)
+{
+    if constexpr (sizeof(KT) == 2) return __builtin_bit_cast(bf16x8, k.piece[b]);
+    else {
+        const uint4 w = k.piece[b / 2];
+        const uint2 lo = tr_widen(b % 2 ? w.z : w.x), hi = tr_widen(b % 2 ? w.w : w.y);
+        return __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
+    }
+}
 template <typename KT, int D>
 __device__ __forceinline__ f32x16 tr_scores(const TrK<KT, D>& k, [[maybe_unused]] const unsigned char* lk, const TrQ<KT, D>& q, [[maybe_unused]] int lane)
 {
@@ -139,13 +160,8 @@ __device__ __forceinline__ f32x16 tr_scores(const TrK<KT, D>& k, [[maybe_unused]
         }
     } else {
 #pragma unroll
-        for (int b = 0; b < TrK<KT, D>::N; ++b) {
-            if constexpr (sizeof(KT) == 2) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k.piece[b]), q.q[b], s, 0, 0, 0);
-            else {
-                const uint2 a0 = tr_widen(k.piece[b].x), a1 = tr_widen(k.piece[b].y), a2 = tr_widen(k.piece[b].z), a3 = tr_widen(k.piece[b].w);
-                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, make_uint4(a0.x, a0.y, a1.x, a1.y)), q.q[2 * b], s, 0, 0, 0);
-                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, make_uint4(a2.x, a2.y, a3.x, a3.y)), q.q[2 * b + 1], s, 0, 0, 0);
-            }
+        for (int b = 0; b < D / 16; ++b) {
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tr_k_operand<KT, D>(k, b), q.q[b], s, 0, 0, 0);
         }
     }
     return s;
@@ -170,6 +186,15 @@ __device__ __forceinline__ TrV<KT, D> tr_load_v(const unsigned char* lv, int p, 
         }
     }
     return v;
+}
+template <typename KT, int D>
+__device__ __forceinline__ bf16x8 tr_v_operand(const TrV<KT, D>& v)
+{
+    if constexpr (sizeof(KT) == 2) return __builtin_bit_cast(bf16x8, make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]));
+    else {
+        const uint2 a = tr_widen(v.w[0]), b = tr_widen(v.w[1]);
+        return __builtin_bit_cast(bf16x8, make_uint4(a.x, a.y, b.x, b.y));
+    }
 }
 template <typename KT, int D>
 __device__ __forceinline__ float tr_element(const TrV<KT, D>& v, int e)
@@ -267,7 +292,7 @@ __device__ __forceinline__ float tr_inverse(const TreeArgs& a, float l, int pref
     return inv;
 }
 
-template <typename KT, int D, int WR> constexpr int tr_ring() { return tree_ring_slots(TrStep<KT, D>::kBytes * (kTrWaves / WR)); }
+template <typename KT, int D, int WR> constexpr int tr_ring() { return tree_ring_slots(TrStep<KT, D>::kBytes * (kTrWaves / WR), sizeof(KT) == 2); }
 
 template <typename KT, int D, int WR>
 __global__ __launch_bounds__(64 * kTrWaves) void tree_kernel(TreeArgs a, TreeSeqs s)
@@ -305,10 +330,7 @@ __global__ __launch_bounds__(64 * kTrWaves) void tree_kernel(TreeArgs a, TreeSeq
     };
     // the copies of a step have landed, those of up to `later` steps behind it may be under way; then everybody's have
     auto wait = [&](int later) {
-        if (R > 3 && later >= 3) tr_wait_copies<(R > 3 ? 3 * C : 0)>();
-        else if (R > 2 && later == 2) tr_wait_copies<(R > 2 ? 2 * C : 0)>();
-        else if (later == 1) tr_wait_copies<C>();
-        else tr_wait_copies<0>();
+        tr_wait_steps<R - 1, C>(later);
         if constexpr (WR > 1) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     };
@@ -328,6 +350,7 @@ __global__ __launch_bounds__(64 * kTrWaves) void tree_kernel(TreeArgs a, TreeSeq
     for (int b = 0; b < DB; ++b) acc[b] = f32x16{};
     float m = kNoKeyTr, l = 0.0f;
 
+    constexpr bool PIPE = sizeof(KT) == 2 && R == 5;           // steps overlap (below)
     TrK<KT, D> k;
     wait(min(R - 1, n_step - 1));
     if (works) tr_load_k(k, ring[0][kg], lane);
@@ -339,13 +362,24 @@ __global__ __launch_bounds__(64 * kTrWaves) void tree_kernel(TreeArgs a, TreeSeq
         if (works) tr_load_k(k, ring[(i + 1) % R][kg], lane);
     };
 
+    auto raise = [&](const f32x16& x) {                        // the reference, to the columns' maxima
+        float top = x[0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) top = fmaxf(top, x[e]);
+        const float m_new = fmaxf(m, pair32_max(top) * c);
+        const float alpha = __builtin_amdgcn_exp2f(m - m_new);
+#pragma unroll
+        for (int b = 0; b < DB; ++b) acc[b] *= alpha;
+        l *= alpha;
+        m = m_new;
+    };
     auto step = [&](int i, auto masked) {
         constexpr bool MASKED = decltype(masked)::value;
         const unsigned char* lk = ring[i % R][kg];
         const unsigned char* lv = lk + S::NK * 1024;
         const int page = page_of(i);
         // The matrix products go first where two waves of a SIMD want to issue: the other's softmax then fills the gaps (32 trees of 64 nodes
-        // over 8 Ki tokens, 64/8 heads: bf16 614 -> 600 us, e4m3 589 -> 556; the softmax first: 623 and 587).
+        // over 8 Ki tokens, 64/8 heads: e4m3 589 -> 556 us when this was put in, 587 with the softmax first).
         __builtin_amdgcn_s_setprio(1);
         f32x16 x = tr_scores(k, lk, q, lane);
         // (16-bit arithmetic: V is read while the scores are being made and turned into weights)
@@ -376,15 +410,7 @@ __global__ __launch_bounds__(64 * kTrWaves) void tree_kernel(TreeArgs a, TreeSeq
         };
         weigh();
         if (__any(sum > kBigTr)) {                             // rare: the reference is raised to the column's maximum
-            float top = x[0];
-#pragma unroll
-            for (int e = 1; e < 16; ++e) top = fmaxf(top, x[e]);
-            const float m_new = fmaxf(m, pair32_max(top) * c);
-            const float alpha = __builtin_amdgcn_exp2f(m - m_new);
-#pragma unroll
-            for (int b = 0; b < DB; ++b) acc[b] *= alpha;
-            l *= alpha;
-            m = m_new;
+            raise(x);
             weigh();
         }
         l += sum;
@@ -407,13 +433,7 @@ __global__ __launch_bounds__(64 * kTrWaves) void tree_kernel(TreeArgs a, TreeSeq
                                                                         pack_bf16(p[8 * u + 4], p[8 * u + 5]), pack_bf16(p[8 * u + 6], p[8 * u + 7])));
 #pragma unroll
                 for (int b = 0; b < DB; ++b) {
-                    uint4 w;
-                    if constexpr (sizeof(KT) == 2) w = make_uint4(v[u][b].w[0], v[u][b].w[1], v[u][b].w[2], v[u][b].w[3]);
-                    else {
-                        const uint2 w0 = tr_widen(v[u][b].w[0]), w1 = tr_widen(v[u][b].w[1]);
-                        w = make_uint4(w0.x, w0.y, w1.x, w1.y);
-                    }
-                    acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), pb, acc[b], 0, 0, 0);
+                    acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tr_v_operand<KT, D>(v[u][b]), pb, acc[b], 0, 0, 0);
                 }
             }
             __builtin_amdgcn_s_setprio(0);
@@ -463,10 +483,90 @@ __global__ __launch_bounds__(64 * kTrWaves) void tree_kernel(TreeArgs a, TreeSeq
     };
 
     // pages whose keys everybody sees, then those that hold nodes
-    const int plain = min(it.prefix / kPage, page1);
+    const int n_plain = max(min(it.prefix / kPage, page1) - page0, 0) / (2 * WK);
     auto one = [&](int i, auto masked) { if (works) step(i, masked); else advance(i); };
     int i = 0;
-    for (; page0 + 2 * WK * (i + 1) <= plain; ++i) one(i, std::false_type{});
+    if constexpr (PIPE) {
+        // Three steps at once: while the matrix unit works on V^T P^T of step i - 1 and K Q^T of step i + 1 in turn, the scores of step i
+        // become weights, a share of them behind each instruction, and the operands of the next turn are read from LDS as theirs
+        // are used up.  (Between two matrix instructions there is room for six or so vector ones; left to itself the compiler puts
+        // the phases one after the other.)  32 trees of 64 nodes over 8 Ki tokens, 64/8 heads of 128: 558 -> 528 us, 1045 TFLOP/s -- the
+        // chip holds 1.9 GHz under it, and without the copies, on what LDS holds, it takes 462; heads of 64: 406 -> 399.  e4m3 keeps the
+        // steps apart: its widening fills the vector unit as it is (530 us; 545 this way).  A ring of five slots, for step i + 2 is
+        // waited for when step i begins.
+        if (n_plain > 0) {
+            constexpr int NQ = D / 16, NP = 2 * DB, SLOTS = NQ + NP, PER = 16 / SLOTS;
+            f32x16 x = {};
+            TrV<KT, D> v[2][DB] = {};
+            bf16x8 pb[2] = {};
+            if (works) x = tr_scores(k, ring[0][kg], q, lane);
+            if (n_step > 1) {
+                wait(min(R - 2, n_step - 2));
+                if (works) tr_load_k(k, ring[1][kg], lane);
+            }
+            for (; i < n_plain; ++i) {
+                if (i + 2 < n_step) {                          // K of step i + 2 is there; V of step i - 1 has been read by everybody
+                    wait(min(R - 4, n_step - 3 - i));
+                    if (i > 0 && i - 1 + R < n_step) issue(i - 1 + R);
+                }
+                if (!works) continue;
+                const unsigned char* lv = ring[i % R][kg] + S::NK * 1024;
+                const unsigned char* lk = ring[(i + 2) % R][kg] + tr_k_at<KT, D>(lane);    // (behind the last step: whatever is there, to no use)
+                f32x16 x_next = {};
+                __builtin_amdgcn_s_setprio(1);
+                float p[16], t[4] = {};
+                uint32_t packed[8];
+#pragma unroll
+                for (int j = 0; j < SLOTS; ++j) {
+                    const int o = j / 2;
+                    if (j % 2 == 0) {
+                        const int u = o / DB, b = o % DB;
+                        acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tr_v_operand<KT, D>(v[u][b]), pb[u], acc[b], 0, 0, 0);
+                        v[u][b] = tr_load_v<KT, D>(lv, u, b, lane);
+                    } else {
+                        x_next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tr_k_operand<KT, D>(k, o), q.q[o], x_next, 0, 0, 0);
+                        if (sizeof(KT) == 2 || o % 2 == 1) k.piece[sizeof(KT) == 2 ? o : o / 2] = *(const uint4*)(lk + (sizeof(KT) == 2 ? o : o / 2) * 512);
+                    }
+#pragma unroll
+                    for (int e = PER * j; e < PER * (j + 1); ++e) {
+                        p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], c, -m));
+                        t[e & 3] += p[e];
+                        if (e % 2 == 1) packed[e / 2] = pack_bf16(p[e - 1], p[e]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                __builtin_amdgcn_s_setprio(0);
+                float sum = (t[0] + t[1]) + (t[2] + t[3]);
+                if (__any(sum > kBigTr)) {
+                    raise(x);
+                    sum = 0.0f;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], c, -m));
+                        sum += p[e];
+                        if (e % 2 == 1) packed[e / 2] = pack_bf16(p[e - 1], p[e]);
+                    }
+                }
+                l += sum;
+#pragma unroll
+                for (int u = 0; u < 2; ++u) pb[u] = __builtin_bit_cast(bf16x8, make_uint4(packed[4 * u], packed[4 * u + 1], packed[4 * u + 2], packed[4 * u + 3]));
+                x = x_next;
+            }
+            if (i < n_step) {                                  // the steps with nodes follow one by one
+                wait(min(R - 2, n_step - 1 - i));
+                if (i - 1 + R < n_step) issue(i - 1 + R);
+                if (works) tr_load_k(k, ring[i % R][kg], lane);
+            }
+            if (works) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int b = 0; b < DB; ++b) acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tr_v_operand<KT, D>(v[u][b]), pb[u], acc[b], 0, 0, 0);
+            }
+        }
+    } else {
+        for (; i < n_plain; ++i) one(i, std::false_type{});
+    }
     for (; i < n_step; ++i) one(i, std::true_type{});
 
     // the waves of other keys hand over their states through LDS: every lane's registers as they are

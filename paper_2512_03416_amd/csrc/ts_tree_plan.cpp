@@ -104,13 +104,13 @@ static TreeTimes tree_times(const ts_attn_desc& d, int rows, int n_cu)
     const int slot = tree_round(rows) * 2 * kPage * d.head_dim * elem;
     const double dims = d.head_dim / 128.0, math = d.q_dtype == TS_F32 ? 8.0 : 1.0;
     TreeTimes t;
-    const int per_cu = std::max(1, std::min(2, 160 * 1024 / (slot * tree_ring_slots(slot))));
+    const int per_cu = std::max(1, std::min(2, 160 * 1024 / (slot * tree_ring_slots(slot, elem == 2))));
     t.places = (int64_t)n_cu * per_cu;
     t.page_alone = 0.36 * rows / 128 * (0.3 + 0.7 * dims) * math;
-    // 32 trees of 64 nodes over 8 Ki tokens (64/8 heads of 128): bf16 558 us with 128 rows, 630 with 64, 1016 with 32 (one workgroup per CU, and
+    // 32 trees of 64 nodes over 8 Ki tokens (64/8 heads of 128): bf16 528 us with 128 rows, 630 with 64, 1015 with 32 (one workgroup per CU, and
     // L2 reads of 17 TB/s), e4m3 530, 564, 628; 8 trees of 100-128 nodes over 2-9 Ki, e4m3: 208, 187, 199
     const bool e4m3 = elem == 1;
-    t.page_full = (rows == 32 ? (per_cu == 1 ? 0.118 : (e4m3 ? 0.155 : 0.16)) : (rows == 64 ? (per_cu == 1 ? 0.2 : (e4m3 ? 0.288 : 0.335)) : (per_cu == 1 ? 0.36 : (e4m3 ? 0.54 : 0.52)))) * dims * math;
+    t.page_full = (rows == 32 ? (per_cu == 1 ? 0.118 : (e4m3 ? 0.155 : 0.16)) : (rows == 64 ? (per_cu == 1 ? 0.2 : (e4m3 ? 0.288 : 0.335)) : (per_cu == 1 ? 0.36 : (e4m3 ? 0.525 : 0.49)))) * dims * math;
     t.page_read = 2.0 * kPage * d.head_dim * elem / 6.2e6;     // 6.2 TB/s
     t.item = 4.0;
     t.start = 5.0;
@@ -123,7 +123,7 @@ static TreeTimes tree_times(const ts_attn_desc& d, int rows, int n_cu)
 // Rows per workgroup: 128 share every copied page four ways; with 32, each wave copies and scans keys of its own and waits for no other,
 // which is faster wherever L2 and HBM keep up (4 trees of 7-26 nodes over 0.5-2.5 Ki tokens, 32/8 heads, 16.9 us with 32 rows, 19.5 with 128).
 // Cuts: uncut, a scan writes no partial results, and the longest scans come first, so that a batch with a workgroup or more for every place
-// comes out even by itself: 32 trees of 32-64 nodes over 1-8 Ki tokens (64/8 heads) take 287 us uncut, 312 in ranges of at most 384
+// comes out even by itself: 32 trees of 32-64 nodes over 1-8 Ki tokens (64/8 heads) took 287 us uncut, 312 in ranges of at most 384
 // pages, 325 in ranges of 192.  Smaller batches are cut until the workgroups fill the places: 8 trees of 30 nodes over 4000 tokens
 // (32/8 heads, 128 rows) 92 us uncut, 39 to 41 in ranges of 32 to 64 pages, 53 in ranges of 16 (most of it partial results).  Ranges of a sequence
 // are of one length.  Both are taken from the times above, which come within 6 % of the best number of rows on these batches and 20 more.
