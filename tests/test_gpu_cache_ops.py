@@ -792,6 +792,20 @@ def test_tree_attention_large_trees(dtype, kind, shape):
         assert (got[0] == 0).all() and (got[b.q_lens[0] - 1] == 0).all()
 
 
+@pytest.mark.parametrize("dtype,kind", KINDS)
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("nodes", [8, 16])
+def test_tree_attention_scans_of_every_length(dtype, kind, dim, nodes):
+    """Prefixes of 0 to 312 tokens in one batch: scans of no step to ten before the steps with nodes.  Queries of four times the size, so
+    that the reference maximum is raised on the way."""
+    n = 40
+    b = Batch((64, 8, dim), dtype, kind, np.full(n, nodes), nodes + 8 * np.arange(n), seed=95)
+    rng = np.random.default_rng(13)
+    see = [tree_see(random_tree(rng, nodes)) for _ in range(n)]
+    q = b.randn(b.T, 64, dim) * 4
+    check(tree_run(b, q, see), *tree_reference(b, q, see))
+
+
 def test_two_graphs_of_one_context():
     """Two captured tree calls, whose scratch is the same, replayed in turn with an eager call between them."""
     batches = [Batch((32, 8, 128), "bf16", "bf16", ql, cl, seed=93 + i) for i, (ql, cl) in enumerate((([12], [4000]), ([30, 7], [2500, 900])))]
