@@ -1,13 +1,16 @@
 """Host side of the rotary append and of the tree attention: frequencies, masks, refusals (no GPU)."""
 import ctypes
 import math
+import os
+import re
+import subprocess
 
 import numpy as np
 import pytest
 
 import paper_2512_03416_amd as ts
 from cache_ops_ref import pack_bits, random_tree, tree_see
-from paper_2512_03416_amd import binding
+from paper_2512_03416_amd import binding, build
 
 
 @pytest.mark.parametrize("rot", [2, 6, 64, 128])
@@ -101,3 +104,26 @@ def test_entry_points_refuse_a_missing_context():
     assert lib.ts_kv_move(null, *[null] * 6, one, one, 1) == binding.TS_ERR_INVALID_ARG
     assert lib.ts_kv_read(null, *[null] * 6, one, one, 1, null, null) == binding.TS_ERR_INVALID_ARG
     assert lib.ts_rope_frequencies(None, null, null) == binding.TS_ERR_INVALID_ARG
+
+
+def test_kernels_keep_their_values_in_registers():
+    """No kernel here spills: two workgroups of the tree attention share a CU at 256 vector registers a lane, and a spilled value next to
+    copies in flight would wait for all of them.  No accumulator registers either: a value parked there while some lanes are masked
+    off is lost to those lanes."""
+    names = set()
+    for src in ("ts_kernels_rope.hip", "ts_kernels_tree.hip"):
+        r = subprocess.run([build.HIPCC] + build.FLAGS + ["-Rpass-analysis=kernel-resource-usage", "-x", "hip", "-c",
+                                                          os.path.join(build.CSRC, src), "-o", os.devnull], capture_output=True, text=True)
+        assert r.returncode == 0, r.stderr[-2000:]
+        name = None
+        for line in r.stderr.splitlines():
+            m = re.search(r"Function Name: (\S+)", line)
+            if m:
+                name = m.group(1)
+                names.add(next((k for k in ("tree_merge_kernel", "tree_kernel", "rope_append_vec_kernel", "rope_append_kernel",
+                                            "kv_read_vec_kernel", "kv_read_kernel", "kv_move_kernel") if k in name), ""))
+            for what, most in (("VGPRs", 256), ("AGPRs", 0), ("VGPRs Spill", 0), (r"ScratchSize \[bytes/lane\]", 0)):
+                m = re.search(r" " + what + r": (\d+)", line)
+                if m and name:
+                    assert int(m.group(1)) <= most, (name, line)
+    assert len(names - {""}) == 7
