@@ -492,7 +492,7 @@ __global__ __launch_bounds__(64 * kTrWaves) void tree_kernel(TreeArgs a, TreeSeq
         // are used up.  (Between two matrix instructions there is room for six or so vector ones; left to itself the compiler puts
         // the phases one after the other.)  32 trees of 64 nodes over 8 Ki tokens, 64/8 heads of 128: 558 -> 528 us, 1045 TFLOP/s -- the
         // chip holds 1.9 GHz under it, and without the copies, on what LDS holds, it takes 462; heads of 64: 406 -> 399.  e4m3 keeps the
-        // steps apart: its widening fills the vector unit as it is (530 us; 545 this way).  A ring of five slots, for step i + 2 is
+        // steps apart: four conversions more per matrix instruction do not fit between two (530 us; 545 this way).  A ring of five slots, for step i + 2 is
         // waited for when step i begins.
         if (n_plain > 0) {
             constexpr int NQ = D / 16, NP = 2 * DB, SLOTS = NQ + NP, PER = 16 / SLOTS;
