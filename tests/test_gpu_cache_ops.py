@@ -875,3 +875,15 @@ def test_refusals_of_addresses_and_rows():
     torch.cuda.synchronize()
     assert (out == 7.0).all() and torch.equal(kc, before[0]) and torch.equal(vc, before[1])
     ctx.close()
+
+
+def test_refusal_of_key_numbers_beyond_int32():
+    """Refused before anything is launched: a tree whose last round of keys has numbers beyond int32."""
+    lib, lens = ts.load_library(), lambda *a: np.asarray(a, np.int32).tobytes()  # noqa: E731
+    t = torch.zeros(64, dtype=torch.int64, device="cuda")
+    p, ctx = t.data_ptr(), ts.Context(ts.Desc.make(2, 1, 64, "bf16", "bf16", 64, 1 << 27))
+    assert lib.ts_tree_attention(ctx._h, 0, p, p, p, 0, 0, p, p, 1, lens(1), lens(2 ** 31 - 1), 1, 0.0, p) == binding.TS_ERR_UNSUPPORTED
+    assert "too large" in ctx.last_error()
+    ctx.close()
+    torch.cuda.synchronize()
+    assert not t.any()
