@@ -209,7 +209,7 @@ int ts_rope_frequencies(const ts_rope_desc *rope, double *freq, double *scale);
 int ts_set_rope(ts_ctx *ctx, const ts_rope_desc *rope);
 
 /* Step a1 with rotary positions: rotates the new tokens' q and K and stores K and V into the paged cache, in one launch per
- * 256 sequences.
+ * 384 sequences.
  *   q, k_new, v_new : DEV, token row t at t * stride elements (slices of one projection's output, say), its heads and dims
  *                     packed [H, D] of q_dtype; stride 0 = packed rows, else at least H * D
  *   q_out : DEV [T, Hq, D], may be q itself if its rows are packed, else must not overlap the inputs; q and q_out may both

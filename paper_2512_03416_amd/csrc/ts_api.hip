@@ -1276,20 +1276,23 @@ int guarded(ts_ctx* c, F&& body)
     }
 }
 
-// The sequences [s0, s0 + n) as kernel arguments; returns the pages that their tokens touch.
-int64_t op_seqs(AppendSeqs* out, const int32_t* lens, const int32_t* prefixes, int64_t row0, int s0, int n)
+// The pages that tokens [prefix, prefix + len) touch.
+int32_t pages_touched(int32_t prefix, int32_t len) { return len > 0 ? (prefix + len - 1) / kPage - prefix / kPage + 1 : 0; }
+// The sequences [s0, s0 + n) as kernel arguments, with so many jobs for a page of a chunk, or of few tokens a page.
+void op_seqs(OpSeqs* out, const int32_t* lens, const int32_t* prefixes, int64_t row0, int s0, int n, int32_t chunk, int32_t few)
 {
-    out->n = n; out->pad0 = out->pad1 = 0;
-    int64_t units = 0, row = row0;
+    out->n = n;
+    int64_t jobs = 0, row = row0;
     for (int i = 0; i < n; ++i) {
-        const int32_t prefix = prefixes ? prefixes[s0 + i] : 0, len = lens[s0 + i];
-        out->seq[i] = AppendSeq{(int32_t)row, prefix, (int32_t)units};
-        if (len > 0) units += (prefix + len - 1) / kPage - prefix / kPage + 1;
+        if (i % 64 == 0) out->first_page[i / 64] = (int32_t)jobs;
+        const int32_t prefix = prefixes ? prefixes[s0 + i] : 0, len = lens[s0 + i], pages = pages_touched(prefix, len);
+        out->seq[i] = OpSeq{(int32_t)row, prefix};
+        jobs += (int64_t)pages * (rope_few(len, pages) ? few : chunk);
         row += len;
     }
-    out->seq[n] = AppendSeq{(int32_t)row, 0, (int32_t)units};
-    out->n_pages = (int32_t)units;
-    return units;
+    out->seq[n] = OpSeq{(int32_t)row, 0};
+    out->n_jobs = (int32_t)jobs;
+    for (int i = (n + 63) / 64; i < kOpSeqs / 64; ++i) out->first_page[i] = (int32_t)jobs;
 }
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
@@ -1370,16 +1373,23 @@ extern "C" int ts_rope_kv_append(ts_ctx* c, void* stream, const void* q, int64_t
         for (int s = 0; s < num_seqs; ++s) if (q_lens[s] > 0) last = s;
         OpGuard og{op};
         int64_t row = 0;
-        for (int s0 = 0; s0 <= last; s0 += kAppendSeqs) {
-            AppendSeqs seqs;
-            const int n = std::min(kAppendSeqs, num_seqs - s0);
-            const int64_t units = op_seqs(&seqs, q_lens, prefix.data(), row, s0, n);
-            row = seqs.seq[n].row0;
-            if (units == 0) continue;
+        for (int s0 = 0; s0 <= last; s0 += kOpSeqs) {
+            OpSeqs seqs;
+            const int n = std::min(kOpSeqs, num_seqs - s0);
+            int64_t pages[2] = {0, 0};                     // of chunks, of few tokens a page
+            for (int i = s0; i < s0 + n; ++i) {
+                const int32_t touched = pages_touched(prefix[i], q_lens[i]);
+                pages[rope_few(q_lens[i], touched)] += touched;
+            }
+            if (pages[0] + pages[1] == 0) continue;
             a.block_table = block_table + (int64_t)s0 * c->desc.max_pages_per_seq;
-            rope_slices(c->desc, row - seqs.seq[0].row0, units, c->opt.n_cu, q != nullptr, &a);
+            a.chunk = rope_slices(c->desc, false, pages[0], c->opt.n_cu, q != nullptr);
+            a.few = rope_slices(c->desc, true, pages[1], c->opt.n_cu, q != nullptr);
+            if (pages[0] * a.chunk.jobs() + pages[1] * a.few.jobs() > INT32_MAX) return fail(c, TS_ERR_UNSUPPORTED, "too many workgroups");
+            op_seqs(&seqs, q_lens, prefix.data(), row, s0, n, a.chunk.jobs(), a.few.jobs());
+            row = seqs.seq[n].row0;
             const hipEvent_t done = last < s0 + n ? op.end : nullptr;
-            const hipError_t e = (hipError_t)timed_launch(c, TS_K_APPEND, true, op.st, [&] { return launch_rope_append(a, seqs, (int32_t)units, stream, done); });
+            const hipError_t e = (hipError_t)timed_launch(c, TS_K_APPEND, true, op.st, [&] { return launch_rope_append(a, seqs, stream, done); });
             if (e != hipSuccess) return hip_fail(c, e, "rotary append launch");
         }
         og.done = true;
@@ -1583,15 +1593,15 @@ extern "C" int ts_kv_read(ts_ctx* c, void* stream, const void* k_cache, const vo
         a.vectors = aligned16(k_out) && aligned16(v_out);
         OpGuard og{op};
         int64_t row = 0;
-        for (int s0 = 0; s0 <= last; s0 += kAppendSeqs) {
-            AppendSeqs seqs;
-            const int n = std::min(kAppendSeqs, num_seqs - s0);
-            const int64_t units = op_seqs(&seqs, lens, starts, row, s0, n);
+        for (int s0 = 0; s0 <= last; s0 += kOpSeqs) {
+            OpSeqs seqs;
+            const int n = std::min(kOpSeqs, num_seqs - s0);
+            op_seqs(&seqs, lens, starts, row, s0, n, 1, 1);
             row = seqs.seq[n].row0;
-            if (units == 0) continue;
+            if (seqs.n_jobs == 0) continue;
             a.block_table = block_table + (int64_t)s0 * c->desc.max_pages_per_seq;
             const hipEvent_t done = last < s0 + n ? op.end : nullptr;
-            const hipError_t e = (hipError_t)timed_launch(c, TS_K_APPEND, true, op.st, [&] { return launch_kv_read(a, seqs, (int32_t)units, stream, done); });
+            const hipError_t e = (hipError_t)timed_launch(c, TS_K_APPEND, true, op.st, [&] { return launch_kv_read(a, seqs, stream, done); });
             if (e != hipSuccess) return hip_fail(c, e, "read launch");
         }
         og.done = true;

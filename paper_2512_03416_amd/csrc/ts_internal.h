@@ -295,7 +295,25 @@ struct Rope {
     double turns[kMaxPairs] = {};
 };
 
-// A launch covers the pages [first_unit, first_unit + units) that its sequences' new tokens (or the tokens to read) touch.
+// Sequences of a launch of the rotary append or the read back, as kernel arguments.  8 bytes each, so that batches of up to 384 take one launch
+// (with 12, as the append has them, 256: 384 decode rows of 64/8 heads took 16.0 us in two launches, 12.3 in one): the pages before a sequence are known every 64
+// sequences, a wave adds up the rest.
+constexpr int kOpSeqs = 384;
+struct OpSeq { int32_t row0, prefix; };    // first token's row (the next entry's row0 ends it), tokens before the first
+struct OpSeqs {
+    int32_t n, n_jobs;                     // jobs: workgroups of the rotary append; pages of the read back
+    int32_t first_page[kOpSeqs / 64];      // (jobs of the) pages that the sequences before number 64 i touch (all of them where there is none)
+    OpSeq seq[kOpSeqs + 1];
+};
+// Workgroups that share a page.
+struct RopeSlices {
+    int32_t q_slices, heads_per_slice;         // its query heads
+    int32_t kv_slices, kv_per_slice;           // its KV heads
+    constexpr int32_t jobs() const { return kv_slices + q_slices; }
+};
+// Few tokens a page: decode rows, as against chunks.
+constexpr bool rope_few(int32_t tokens, int32_t pages) { return tokens < 2 * pages; }
+// A launch covers the pages that its sequences' new tokens (or the tokens to read) touch, from job (or page) first_unit on.
 struct RopeArgs {
     Geometry geo;
     const void* q; const void* k; const void* v;
@@ -305,13 +323,12 @@ struct RopeArgs {
     const float* k_scale; const float* v_scale;
     const int32_t* block_table;        // of the launch's first sequence
     const int32_t* positions;
-    int32_t q_slices, heads_per_slice; // workgroups that share a page's query heads
-    int32_t kv_slices, kv_per_slice;   // ... its KV heads
+    RopeSlices chunk, few;             // pages of chunks; of sequences with few tokens a page
     int32_t vectors;                   // bases and strides are multiples of 16 bytes
     int32_t first_unit;
     Rope rope;
 };
-static_assert(sizeof(RopeArgs) + sizeof(AppendSeqs) <= 4096, "kernel arguments");
+static_assert(sizeof(RopeArgs) + sizeof(OpSeqs) <= 4096, "kernel arguments");
 
 struct MoveArgs {
     Geometry geo;
@@ -392,8 +409,8 @@ constexpr int tree_ring_slots(int slot_bytes, bool bf16)
     return fit < 2 ? 2 : (fit > most ? most : fit);
 }
 
-// Heads that one workgroup of the rotary append takes of a page's tokens (RopeArgs).
-void rope_slices(const ts_attn_desc& d, int64_t tokens, int64_t units, int n_cu, bool with_q, RopeArgs* a);
+// Heads that one workgroup of the rotary append takes of a page's tokens.
+RopeSlices rope_slices(const ts_attn_desc& d, bool few, int64_t pages, int n_cu, bool with_q);
 int rope_frequencies(const ts_rope_desc* r, double* freq, double* scale, std::string* err);
 
 // Launchers (defined in the .hip files).  All return a hipError_t cast to int.  done: a hipEvent_t recorded at the end of
@@ -413,8 +430,8 @@ int launch_prefill(const AttnArgs& a, void* stream, void* done);
 int launch_mixed(const AttnArgs& a, void* stream, void* done);
 int launch_prefill_resident(const AttnArgs& a, void* stream, void* done);
 int launch_prefill_combine(const AttnArgs& a, void* stream, void* done);
-int launch_rope_append(const RopeArgs& a, const AppendSeqs& s, int32_t units, void* stream, void* done);
-int launch_kv_read(const ReadArgs& a, const AppendSeqs& s, int32_t units, void* stream, void* done);
+int launch_rope_append(const RopeArgs& a, const OpSeqs& s, void* stream, void* done);
+int launch_kv_read(const ReadArgs& a, const OpSeqs& s, void* stream, void* done);
 int launch_kv_move(const MoveArgs& a, const MoveSeqs& s, void* stream, void* done);
 int launch_check_pages(const PageCheck& p, const int32_t* block_table, int max_pages, int64_t num_pages, int32_t* result, void* stream);
 int launch_tree(const TreeArgs& a, const TreeSeqs& s, int64_t items, void* stream, void* done);

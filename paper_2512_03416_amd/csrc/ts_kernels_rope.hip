@@ -30,26 +30,40 @@ __device__ __forceinline__ f32x2 rotated(float x, float y, f32x2 c, bool turns)
     return f32x2{__builtin_fmaf(x, c.x, -(y * c.y)), __builtin_fmaf(y, c.x, x * c.y)};
 }
 
-// The sequence that page number u of the launch belongs to (a sequence without new tokens shares the number of the next one:
-// the last match counts).
-__device__ __forceinline__ int seq_of_page(const AppendSeqs& s, int u)
+// The sum over the lanes up to this one.
+__device__ __forceinline__ int sum_up_to_lane(int x)
 {
-    const int lane = threadIdx.x & 63;
-    int i = -1;
-#pragma unroll
-    for (int b = 0; b < kAppendSeqs; b += 64)
-        i += __builtin_popcountll(__ballot(b + lane < s.n && s.seq[min(b + lane, kAppendSeqs - 1)].first_page <= u));
-    return i;
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);     // within rows of 16: from 1, 2, 4, 8 lanes before
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);    // rows 1 and 3: the last lane of the row before
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);    // rows 2 and 3: lane 31
+    return x;
 }
 
-// One page's share of a sequence's tokens: slots [lo, hi) hold rows row_slot0 + slot.
-struct PageRun { int seq, page_idx, lo, hi, row_slot0; };
-__device__ __forceinline__ PageRun page_run(const AppendSeqs& s, int u)
+// The sequence and the page of it that job number u of the launch belongs to: slots [lo, hi) of the page hold rows row_slot0 + slot.  A page
+// has `few` or `chunk` jobs, of which this is number `job`.
+struct PageRun { int seq, page_idx, lo, hi, row_slot0, job; bool few; };
+__device__ __forceinline__ PageRun page_run(const OpSeqs& s, int u, int chunk, int few)
 {
-    const int i = seq_of_page(s, u);
-    const AppendSeq q = s.seq[i];
-    const int n = s.seq[i + 1].row0 - q.row0, page = (q.prefix >> 4) + u - q.first_page;
-    return PageRun{i, page, max(q.prefix - page * kPage, 0), min(q.prefix + n - page * kPage, kPage), q.row0 + page * kPage - q.prefix};
+    int b = 0, before = 0;                                 // the last 64 sequences that begin at u or earlier
+#pragma unroll
+    for (int k = 1; k < kOpSeqs / 64; ++k)
+        if (s.first_page[k] <= u) { b = k; before = s.first_page[k]; }
+    const int i = b * 64 + (int)(threadIdx.x & 63), at = min(i, s.n - 1);
+    struct { int row0, prefix, next; } q;                  // (the next entry's row0: one load of 12 bytes)
+    __builtin_memcpy(&q, &s.seq[at], sizeof q);
+    const int len = i < s.n ? q.next - q.row0 : 0;
+    const int pages = len > 0 ? ((q.prefix + len - 1) >> 4) - (q.prefix >> 4) + 1 : 0;
+    const int per = rope_few(len, pages) ? few : chunk, jobs = pages * per;
+    const int end = before + sum_up_to_lane(jobs);
+    const int lane = __builtin_ctzll(__ballot(pages > 0 && end > u));      // (the first whose jobs reach beyond u)
+    auto of = [&](int v) { return __builtin_amdgcn_readlane(v, lane); };
+    const int prefix = of(q.prefix), n = of(len), row0 = of(q.row0), j = u - of(end - jobs), of_page = of(per);
+    const int page = (prefix >> 4) + j / of_page;
+    return PageRun{b * 64 + lane, page, max(prefix - page * kPage, 0), min(prefix + n - page * kPage, kPage), row0 + page * kPage - prefix,
+                   j % of_page, rope_few(n, of(pages))};
 }
 
 template <typename T> __device__ __forceinline__ float load_float(const T* p)
@@ -73,15 +87,15 @@ template <typename CT> __device__ __forceinline__ CT to_cache(float f, float sca
 // ST: element type of the new tokens (float, or uint16_t for bf16 bits), CT: of the cache.
 // A workgroup takes one page's new tokens: of one KV head (K rotated, V, both into the cache), or of some query heads.
 template <typename ST, typename CT, int D>
-__global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a, AppendSeqs s)
+__global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a, OpSeqs s)
 {
     constexpr int P = D / 2;
     __shared__ f32x2 turn[kPage][P];
     __shared__ ST rows[kPage][D + 4 / (int)sizeof(ST)];
     const int Hkv = a.geo.Hkv, Hq = a.geo.Hq;
-    const int per = a.kv_slices + a.q_slices;
-    const int u = a.first_unit + (int)blockIdx.x / per, job = blockIdx.x % per;
-    const PageRun r = page_run(s, u);
+    const PageRun r = page_run(s, a.first_unit + (int)blockIdx.x, a.chunk.jobs(), a.few.jobs());
+    const RopeSlices sl = r.few ? a.few : a.chunk;
+    const int job = r.job;
     const int tid = threadIdx.x, n_tok = r.hi - r.lo, row0 = r.row_slot0 + r.lo;
     const int half = a.rope.rot_dim / 2;
     for (int i = tid; i < n_tok * P; i += 256) {
@@ -96,8 +110,8 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a, AppendSeqs
         else { x = p; y = p + half; }
     };
     __syncthreads();
-    if (job >= a.kv_slices) {
-        const int h0 = (job - a.kv_slices) * a.heads_per_slice, h1 = min(h0 + a.heads_per_slice, Hq), nh = h1 - h0;
+    if (job >= sl.kv_slices) {
+        const int h0 = (job - sl.kv_slices) * sl.heads_per_slice, h1 = min(h0 + sl.heads_per_slice, Hq), nh = h1 - h0;
         for (int i = tid; i < n_tok * nh * P; i += 256) {
             const int p = i % P, h = h0 + i / P % nh, t = i / P / nh;
             const ST* q = (const ST*)a.q + (row0 + t) * a.q_stride + h * D;
@@ -112,7 +126,7 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a, AppendSeqs
     }
     const int64_t page = a.block_table[(int64_t)r.seq * a.geo.max_pages + r.page_idx];
     constexpr int X = 16 / (int)sizeof(CT);
-    for (int g = job * a.kv_per_slice; g < min((job + 1) * a.kv_per_slice, Hkv); ++g) {
+    for (int g = job * sl.kv_per_slice; g < min((job + 1) * sl.kv_per_slice, Hkv); ++g) {
         const int64_t tile = tile_elem_base(page, Hkv, g, D);
         CT* kt = (CT*)a.k_cache + tile;
         CT* vt = (CT*)a.v_cache + tile;
@@ -143,9 +157,9 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a, AppendSeqs
 // The same in 16-byte pieces (bases and strides that allow it; with TS_ROPE_HALF rot_dim / 2 has to be whole pieces).  A thread takes a
 // unit of X pairs (X = elements of a piece) of one token -- two pieces, which hold the pairs' two sides, or X pairs side by side -- and
 // keeps their angles in registers while it goes through the heads; the angles are worked out once per workgroup, in LDS.
-// What bounds it: memory.  34 188 tokens (64/8 heads of 128, bf16, 1.40 GB read and written): 296 us, 4.7 TB/s of the 5.1 that a large copy
-// reaches.  Stores carry the non-temporal hint (310 us without; 2024 tokens of 40/8 heads 14.1 -> 12.8), loads do not: with it the
-// large append takes 283 us, but inputs that the projection has just left in the caches come from memory (2024 tokens 18.4 us).
+// What bounds it: memory.  34 188 tokens (64/8 heads of 128, bf16, 1.40 GB read and written): 284 us, 4.9 TB/s where a large copy
+// reaches 4.7 to 5.1.  Stores carry the non-temporal hint (in two launches 296 us, 310 without; 2024 tokens of 40/8 heads 14.1 -> 12.8), loads
+// do not: with it the large append took 283 us instead of 296, but inputs that the projection has just left in the caches come from memory (2024 tokens 18.4 us).
 template <typename ST> struct RopePiece { static constexpr int X = 16 / (int)sizeof(ST); float v[X]; };
 template <typename ST>
 __device__ __forceinline__ RopePiece<ST> piece_of(uint4 w)
@@ -179,16 +193,16 @@ __device__ __forceinline__ uint32_t e4m3_word(float a, float b, float c, float d
 }
 
 template <typename ST, typename CT, int D>
-__global__ __launch_bounds__(256) void rope_append_vec_kernel(RopeArgs a, AppendSeqs s)
+__global__ __launch_bounds__(256) void rope_append_vec_kernel(RopeArgs a, OpSeqs s)
 {
     constexpr int P = D / 2, X = 16 / (int)sizeof(ST), U = P / X;     // pairs of a head, of a unit; units of a head
     constexpr int kPad = D + X;                                       // LDS row of V: other banks for the next slot
     __shared__ __align__(16) f32x2 turn[kPage][P];
     __shared__ __align__(16) ST vrow[kPage][kPad];
     const int Hkv = a.geo.Hkv, Hq = a.geo.Hq;
-    const int per = a.kv_slices + a.q_slices;
-    const int u0 = a.first_unit + (int)blockIdx.x / per, job = blockIdx.x % per;
-    const PageRun r = page_run(s, u0);
+    const PageRun r = page_run(s, a.first_unit + (int)blockIdx.x, a.chunk.jobs(), a.few.jobs());
+    const RopeSlices sl = r.few ? a.few : a.chunk;
+    const int job = r.job;
     const int tid = threadIdx.x, n_tok = r.hi - r.lo, row0 = r.row_slot0 + r.lo;
     const int half = a.rope.rot_dim / 2;
     const bool inter = a.rope.interleaved;
@@ -197,9 +211,9 @@ __global__ __launch_bounds__(256) void rope_append_vec_kernel(RopeArgs a, Append
     const int t = mine / U, u = mine % U;
     const bool paired = !inter && u * X < half;                       // two sides of X pairs; else 2 X dims side by side
     const int d0 = paired || inter ? (inter ? 2 : 1) * u * X : 2 * u * X, d1 = paired ? d0 + half : d0 + X;
-    const bool is_q = job >= a.kv_slices;
-    const int h0 = is_q ? (job - a.kv_slices) * a.heads_per_slice : job * a.kv_per_slice;
-    const int h1 = is_q ? min(h0 + a.heads_per_slice, Hq) : min(h0 + a.kv_per_slice, Hkv);
+    const bool is_q = job >= sl.kv_slices;
+    const int h0 = is_q ? (job - sl.kv_slices) * sl.heads_per_slice : job * sl.kv_per_slice;
+    const int h1 = is_q ? min(h0 + sl.heads_per_slice, Hq) : min(h0 + sl.kv_per_slice, Hkv);
     const ST* src = is_q ? (const ST*)a.q + (row0 + t) * a.q_stride : (const ST*)a.k + (row0 + t) * a.k_stride;
     const bool active = first < step;
     int h = h0 + first;
@@ -331,7 +345,7 @@ __global__ __launch_bounds__(256) void rope_append_vec_kernel(RopeArgs a, Append
 }
 
 template <typename ST, typename CT>
-static int launch_rope_d(const RopeArgs& a, const AppendSeqs& s, int64_t blocks, hipStream_t st, hipEvent_t done)
+static int launch_rope_d(const RopeArgs& a, const OpSeqs& s, int64_t blocks, hipStream_t st, hipEvent_t done)
 {
     const dim3 grid((unsigned)blocks);
     const bool vec = a.vectors && (a.rope.interleaved || (a.rope.rot_dim / 2) % (16 / (int)sizeof(ST)) == 0);
@@ -343,22 +357,20 @@ static int launch_rope_d(const RopeArgs& a, const AppendSeqs& s, int64_t blocks,
     return launch_kernel(rope_append_kernel<ST, CT, 64>, grid, dim3(256), st, done, a, s);
 }
 
-int launch_rope_append(const RopeArgs& a, const AppendSeqs& s, int32_t units, void* stream, void* done)
+int launch_rope_append(const RopeArgs& a, const OpSeqs& s, void* stream, void* done)
 {
     if (a.geo.D != 128 && a.geo.D != 64) return (int)hipErrorInvalidValue;
     RopeArgs part = a;
-    const int per = a.kv_slices + a.q_slices;
-    const int64_t most = kMaxWorkgroups / per;
-    if (most < 1) return (int)hipErrorInvalidValue;
+    const int64_t units = s.n_jobs, most = kMaxWorkgroups;
     for (int64_t u = 0; u < units; u += most) {
         const int64_t n = units - u < most ? units - u : most;
         part.first_unit = (int32_t)u;
         hipStream_t st = (hipStream_t)stream;
         hipEvent_t ev = u + n < units ? nullptr : (hipEvent_t)done;
         int e;
-        if (a.geo.q_dtype == TS_F32) e = launch_rope_d<float, float>(part, s, n * per, st, ev);
-        else if (a.geo.kv_dtype == TS_BF16) e = launch_rope_d<uint16_t, uint16_t>(part, s, n * per, st, ev);
-        else e = launch_rope_d<uint16_t, uint8_t>(part, s, n * per, st, ev);
+        if (a.geo.q_dtype == TS_F32) e = launch_rope_d<float, float>(part, s, n, st, ev);
+        else if (a.geo.kv_dtype == TS_BF16) e = launch_rope_d<uint16_t, uint16_t>(part, s, n, st, ev);
+        else e = launch_rope_d<uint16_t, uint8_t>(part, s, n, st, ev);
         if (e != (int)hipSuccess) return e;
     }
     return (int)hipSuccess;
@@ -366,11 +378,11 @@ int launch_rope_append(const RopeArgs& a, const AppendSeqs& s, int32_t units, vo
 
 // Reading back: a workgroup takes one page of one KV head.  Element by element, for outputs on any address:
 template <typename CT, typename OT, int D>
-__global__ __launch_bounds__(256) void kv_read_kernel(ReadArgs a, AppendSeqs s)
+__global__ __launch_bounds__(256) void kv_read_kernel(ReadArgs a, OpSeqs s)
 {
     const int Hkv = a.geo.Hkv;
     const int u = a.first_unit + (int)blockIdx.x / Hkv, g = blockIdx.x % Hkv;
-    const PageRun r = page_run(s, u);
+    const PageRun r = page_run(s, u, 1, 1);
     const int64_t tile = tile_elem_base(a.block_table[(int64_t)r.seq * a.geo.max_pages + r.page_idx], Hkv, g, D);
     constexpr int X = 16 / (int)sizeof(CT);
     const CT* kt = (const CT*)a.k_cache + tile;
@@ -398,7 +410,7 @@ __global__ __launch_bounds__(256) void kv_read_kernel(ReadArgs a, AppendSeqs s)
 // LDS.  What bounds it: memory.  108 951 tokens of an e4m3 cache (64/8 heads of 128, 0.22 GB read, 0.45 written): 129 us, 5.2 TB/s, 166
 // without the non-temporal hint on the stores; loads with it 154.
 template <typename CT, typename OT, int D>
-__global__ __launch_bounds__(256) void kv_read_vec_kernel(ReadArgs a, AppendSeqs s)
+__global__ __launch_bounds__(256) void kv_read_vec_kernel(ReadArgs a, OpSeqs s)
 {
     constexpr int X = 16 / (int)sizeof(CT), C = D / X, PER = kPage / X;   // elements of a piece; K pieces of a token; V pieces of a dim
     constexpr int W = 16 / (int)sizeof(OT), kPad = D + W;
@@ -406,10 +418,10 @@ __global__ __launch_bounds__(256) void kv_read_vec_kernel(ReadArgs a, AppendSeqs
     __shared__ __align__(16) OT rows[kPage][kPad];
     const int Hkv = a.geo.Hkv, tid = threadIdx.x;
     // (workgroup i runs on die i % 8: a page's heads, whose rows lie next to each other, go to one die; over three caches in turn 156.2 ->
-    // 153.4 us.  The same for the append changes nothing, 294 us, or costs 2 %, drafted trees)
-    const int u = a.first_unit + (int)blockIdx.x / (8 * Hkv) * 8 + (int)blockIdx.x % 8, g = blockIdx.x / 8 % Hkv;
-    if (u >= s.n_pages) return;
-    const PageRun r = page_run(s, u);
+    // 153.4 us when this was put in.  The same for the append changes nothing, 294 us, or costs 2 %, drafted trees)
+    const int w = (int)(blockIdx.x / 8), g = w % Hkv, u = a.first_unit + w / Hkv * 8 + (int)blockIdx.x % 8;
+    if (u >= s.n_jobs) return;
+    const PageRun r = page_run(s, u, 1, 1);
     const int64_t tile = tile_elem_base(a.block_table[(int64_t)r.seq * a.geo.max_pages + r.page_idx], Hkv, g, D);
     const CT* kt = (const CT*)a.k_cache + tile;
     const CT* vt = (const CT*)a.v_cache + tile;
@@ -470,14 +482,15 @@ __global__ __launch_bounds__(256) void kv_read_vec_kernel(ReadArgs a, AppendSeqs
 }
 
 template <typename CT, typename OT, int D>
-static int launch_read_d(const ReadArgs& a, const AppendSeqs& s, dim3 grid, hipStream_t st, hipEvent_t done)
+static int launch_read_d(const ReadArgs& a, const OpSeqs& s, dim3 grid, hipStream_t st, hipEvent_t done)
 {
     if (a.vectors) return launch_kernel(kv_read_vec_kernel<CT, OT, D>, grid, dim3(256), st, done, a, s);
     return launch_kernel(kv_read_kernel<CT, OT, D>, grid, dim3(256), st, done, a, s);
 }
 
-int launch_kv_read(const ReadArgs& a, const AppendSeqs& s, int32_t units, void* stream, void* done)
+int launch_kv_read(const ReadArgs& a, const OpSeqs& s, void* stream, void* done)
 {
+    const int64_t units = s.n_jobs;
     if (a.geo.D != 128 && a.geo.D != 64) return (int)hipErrorInvalidValue;
     ReadArgs part = a;
     const int64_t most = kMaxWorkgroups / a.geo.Hkv / 8 * 8;

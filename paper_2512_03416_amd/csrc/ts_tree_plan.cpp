@@ -68,17 +68,18 @@ int rope_frequencies(const ts_rope_desc* r, double* freq, double* scale, std::st
 
 // A page's angles are worked out by every workgroup that takes a share of its heads: as many heads as leave the GPU full.  Decode rows
 // are pages of one token, of which a workgroup takes more where there are many: 256 rows (64/8 heads of 128) 15.1 us in 2304 workgroups,
-// 7.7 in 512.
-void rope_slices(const ts_attn_desc& d, int64_t tokens, int64_t units, int n_cu, bool with_q, RopeArgs* a)
+// 7.7 in 512.  Chunks of the same launch go by their own rule (258 rows next to a chunk of 22 tokens, 40/8 heads: 12.6 us; all by the rows' rule 32.6).
+RopeSlices rope_slices(const ts_attn_desc& d, bool few, int64_t pages, int n_cu, bool with_q)
 {
-    const bool rows = tokens < 2 * units;
-    const int64_t enough = (int64_t)n_cu * (rows ? 2 : 8);
-    a->kv_per_slice = rows && units * d.num_kv_heads > enough ? std::min(8, d.num_kv_heads) : 1;
-    a->kv_slices = (d.num_kv_heads + a->kv_per_slice - 1) / a->kv_per_slice;
+    const int64_t enough = (int64_t)n_cu * (few ? 2 : 8);
+    RopeSlices r;
+    r.kv_per_slice = few && pages * d.num_kv_heads > enough ? std::min(8, d.num_kv_heads) : 1;
+    r.kv_slices = (d.num_kv_heads + r.kv_per_slice - 1) / r.kv_per_slice;
     int32_t heads = d.num_q_heads;
-    while (heads > 8 && units * (a->kv_slices + (d.num_q_heads + heads - 1) / heads) < enough) heads = (heads + 1) / 2;
-    a->heads_per_slice = heads;
-    a->q_slices = with_q ? (d.num_q_heads + heads - 1) / heads : 0;
+    while (heads > 8 && pages * (r.kv_slices + (d.num_q_heads + heads - 1) / heads) < enough) heads = (heads + 1) / 2;
+    r.heads_per_slice = heads;
+    r.q_slices = with_q ? (d.num_q_heads + heads - 1) / heads : 0;
+    return r;
 }
 
 // Times of the tree kernel in us, measured, from which its rows per workgroup and its cuts are chosen.

@@ -793,6 +793,18 @@ def test_tree_attention_large_trees(dtype, kind, shape):
 
 
 @pytest.mark.parametrize("dtype,kind", KINDS)
+@pytest.mark.parametrize("offset", [0, 1])
+def test_rope_append_rows_next_to_chunks(dtype, kind, offset):
+    """Pages with one token and whole pages in one launch, which share their heads out differently; sequences behind the first launch's."""
+    rng = np.random.default_rng(14)
+    ql = np.ones(420, int)
+    ql[[0, 130, 131, 400]] = 37, 22, 0, 50
+    ql[300:340] = 0
+    b = Batch((20, 5, 128), dtype, kind, ql, ql + rng.integers(0, 60, 420), seed=96)
+    rope_case(b, dict(rot_dim=128, base=1e6), b.randn(b.T, 20, 128), b.randn(b.T, 5, 128), b.randn(b.T, 5, 128), strided=True, positions=None, offset=offset)
+
+
+@pytest.mark.parametrize("dtype,kind", KINDS)
 @pytest.mark.parametrize("dim", [64, 128])
 @pytest.mark.parametrize("nodes", [8, 16])
 def test_tree_attention_scans_of_every_length(dtype, kind, dim, nodes):
