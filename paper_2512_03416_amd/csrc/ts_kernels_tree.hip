@@ -311,7 +311,6 @@ __global__ __launch_bounds__(64 * kTrWaves) void tree_kernel(TreeArgs a, TreeSeq
     const int page0 = it.part * it.part_pages, page1 = min(page0 + it.part_pages, pages);
     const int n_step = (page1 - page0 + 2 * WK - 1) / (2 * WK);
     const int first_row = it.group * ROWS + wr * 32;
-    const bool works = first_row < it.node_rows;               // (a wave without rows only copies)
 
     const int32_t TS_CONSTANT* bt = as_constant(a.block_table) + (int64_t)it.seq * a.geo.max_pages;
     const char* kc = (const char*)a.k_cache + (int64_t)it.g * S::PB;
@@ -321,6 +320,7 @@ __global__ __launch_bounds__(64 * kTrWaves) void tree_kernel(TreeArgs a, TreeSeq
     // (past the end of the range: its last page again, whose keys do not count a second time)
     auto page_of = [&](int i) { return page0 + 2 * (WK * i + kg); };
     auto id_of = [&](int page) { return bt[min(page, page1 - 1)]; };
+    const bool works = first_row < it.node_rows && page_of(0) < page1;     // (a wave without rows or keys only copies)
     // (page ids are asked for a step ahead; the opaque copies keep the wait for them where they are used)
     int32_t next0 = id_of(page_of(0)), next1 = id_of(page_of(0) + 1);
     auto issue = [&](int i) {

@@ -91,6 +91,8 @@ struct TreeTimes {
     int64_t places;                    // workgroups resident at once
     double item;                       // a workgroup's fixed share of its CU: 29 trees of 16 nodes over 10 tokens (64/8 heads) take 10.7 us in 232
                                        // workgroups of 128 rows, 14.9 in 464 of 64, 28 in 928 of 32
+    double alone;                      // ... and its least time: 35 trees of 2-6 nodes over 0-5 tokens (40/8 heads, bf16), 280 workgroups, take 14.3 us
+                                       // with 32 rows (256 places), 9.3 with 64
     double start, round;               // launch, page ids, queries, first copies, last stores; of a later workgroup in the same place
     double merge, merge_row;           // merge launch, and a partial row written and read again
 };
@@ -114,6 +116,7 @@ static TreeTimes tree_times(const ts_attn_desc& d, int rows, int n_cu)
     t.page_full = (rows == 32 ? (per_cu == 1 ? 0.118 : (e4m3 ? 0.155 : 0.16)) : (rows == 64 ? (per_cu == 1 ? 0.2 : (e4m3 ? 0.288 : 0.335)) : (per_cu == 1 ? 0.36 : (e4m3 ? 0.525 : 0.49)))) * dims * math;
     t.page_read = 2.0 * kPage * d.head_dim * elem / 6.2e6;     // 6.2 TB/s
     t.item = 4.0;
+    t.alone = 4.6;
     t.start = 5.0;
     t.round = 2.5;
     t.merge = 6.0;
@@ -168,7 +171,9 @@ void plan_tree(const ts_attn_desc& d, const int32_t* q_lens, const int32_t* ctx_
     double best_time = 0.0;
     for (int rows_wg = 128; rows_wg >= 32; rows_wg /= 2) {
         if (!tree_rows_fit(d, rows_wg)) break;
-        if (rows_wg > 32 && tree_rows_fit(d, rows_wg / 2) && most <= rows_wg / 2) continue;   // (half of the rows would be empty everywhere)
+        // (half of the rows would be empty everywhere: only where workgroups of half as many need more than one round of places)
+        if (rows_wg > 32 && tree_rows_fit(d, rows_wg / 2) && most <= rows_wg / 2 &&
+            (int64_t)plan->seqs.size() * Hkv <= tree_times(d, rows_wg / 2, n_cu).places) continue;
         const TreeTimes t = tree_times(d, rows_wg, n_cu);
         const int32_t round = tree_round(rows_wg), whole = (longest + round - 1) / round * round;
         auto groups_of = [&](const TreeSeq& s) { return tree_groups(s.n_nodes, G, rows_wg); };
@@ -202,7 +207,7 @@ void plan_tree(const ts_attn_desc& d, const int32_t* q_lens, const int32_t* ctx_
                 time = std::max(time, 0.85 * (len * t.page_alone + ranges[k].first * std::max(0.0, t.page_full - t.page_alone)));
             }
             if (items > t.places) time += 0.15 * page * total * Hkv / items + ((double)items / t.places - 1.0) * t.round;
-            time = t.start + std::max({time, reads * Hkv * t.page_read, (double)items / n_cu * t.item});
+            time = t.start + std::max({time, reads * Hkv * t.page_read, (double)items / n_cu * t.item, (double)((items + t.places - 1) / t.places) * t.alone});
             if (rows > 0) time += t.merge + rows * t.merge_row;
             if (best == 0 || time < best_time) { plan->rows = rows_wg; best = L; best_time = time; }
             if (items > 4 * t.places) break;
