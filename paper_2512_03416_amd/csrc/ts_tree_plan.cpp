@@ -130,7 +130,7 @@ static TreeTimes tree_times(const ts_attn_desc& d, int rows, int n_cu)
 // comes out even by itself: 32 trees of 32-64 nodes over 1-8 Ki tokens (64/8 heads) took 287 us uncut, 312 in ranges of at most 384
 // pages, 325 in ranges of 192.  Smaller batches are cut until the workgroups fill the places: 8 trees of 30 nodes over 4000 tokens
 // (32/8 heads, 128 rows) 92 us uncut, 39 to 41 in ranges of 32 to 64 pages, 53 in ranges of 16 (most of it partial results).  Ranges of a sequence
-// are of one length.  Both are taken from the times above, which come within 6 % of the best number of rows on these batches and 20 more.
+// are of one length.  Both are taken from the times above, which come within 8 % of the best number of rows on these batches and 22 more.
 void plan_tree(const ts_attn_desc& d, const int32_t* q_lens, const int32_t* ctx_lens, int num_seqs, int n_cu, TreePlan* plan)
 {
     const int32_t G = d.num_q_heads / d.num_kv_heads, Hkv = d.num_kv_heads;
