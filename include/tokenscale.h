@@ -236,8 +236,8 @@ int ts_rope_kv_append(ts_ctx *ctx, void *stream,
  *               (mask_words is not read)
  *   other arguments as in ts_mixed_paged_attention; q [T, Hq, D] and out [T, Hq, D] must be 16-byte aligned and not overlap
  * What a row does not see has no influence on it, whatever its value (infinities and NaN included).  A row whose visible
- * scores are all -inf is NaN.  Softmax statistics and sums are held in single precision, the weights enter the second
- * product in q_dtype.  Results are run-to-run identical.
+ * scores are all -inf is NaN.  Softmax statistics and sums are held in single precision; the weights are rounded to q_dtype,
+ * above and below the quotient alike.  Results are run-to-run identical.
  * Errors: TS_ERR_INVALID_ARG as above and for too few mask words; TS_ERR_UNSUPPORTED for more than TS_TREE_MAX_NODES nodes. */
 #define TS_TREE_MAX_NODES 256
 int ts_tree_attention(ts_ctx *ctx, void *stream,

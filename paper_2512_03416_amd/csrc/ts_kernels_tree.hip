@@ -14,6 +14,10 @@
 //   - The masks are looked at on the pages that hold nodes only.
 // The running maximum is a reference in log2 units that is raised only when a step's weights add up to more than 2^16 in some lane:
 // any reference gives the same quotient, and the maximum itself is not needed for as long.
+// Weights are rounded to q's type, which the second product's matrix instruction takes (in two parts, so that nothing is lost, it would be run
+// twice), and the sum below the quotient is that of the rounded ones: where many keys have one score their weights are all rounded alike, by
+// up to 2^-8, and a sum of the unrounded ones would leave that in the result.  32 trees of 64 nodes over 8 Ki tokens, 64/8 heads of 128, take 564 us,
+// 543 with the other sum (e4m3 557 and 550; heads of 64 228 and 229, e4m3 193 and 220).
 #include <type_traits>
 
 #include "ts_device.h"
@@ -221,6 +225,11 @@ __device__ __forceinline__ bool tr_clean_v(TrV<KT, D>& v, int have)
 }
 
 __device__ __forceinline__ uint32_t pack_bf16(float x, float y) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, bf16x2)); }
+// sum + both of a pair of bf16, in single precision (measured over 16 Ki random triples: at most 2.5 x 2^-24 short of the exact sum).
+__device__ __forceinline__ float add_pair(uint32_t pair, float sum)
+{
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3f803f80u), sum, false);
+}
 
 // Which of the eight keys from node number j0 on a node sees, as bits 0 .. 7.  Negative numbers are the prefix, which everybody sees;
 // nodes from n_nodes on do not exist.  Without a mask a node sees those up to itself.
@@ -400,12 +409,21 @@ __global__ __launch_bounds__(64 * kTrWaves) void tree_kernel(TreeArgs a, TreeSeq
             for (int e = 0; e < 16; ++e) x[e] = seen >> e & 1 ? x[e] : -INFINITY;
         }
         float p[16], sum;
+        [[maybe_unused]] uint32_t packed[8];                   // (16-bit arithmetic) the weights as they enter the second product
         auto weigh = [&] {
 #pragma unroll
             for (int e = 0; e < 16; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], c, -m));
             float t[4];
+            if constexpr (F32) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) t[e] = (p[e] + p[e + 4]) + (p[e + 8] + p[e + 12]);
+                for (int e = 0; e < 4; ++e) t[e] = (p[e] + p[e + 4]) + (p[e + 8] + p[e + 12]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    packed[e] = pack_bf16(p[2 * e], p[2 * e + 1]);
+                    t[e & 3] = add_pair(packed[e], e < 4 ? 0.0f : t[e & 3]);
+                }
+            }
             sum = (t[0] + t[1]) + (t[2] + t[3]);
         };
         weigh();
@@ -429,8 +447,7 @@ __global__ __launch_bounds__(64 * kTrWaves) void tree_kernel(TreeArgs a, TreeSeq
             __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const bf16x8 pb = __builtin_bit_cast(bf16x8, make_uint4(pack_bf16(p[8 * u], p[8 * u + 1]), pack_bf16(p[8 * u + 2], p[8 * u + 3]),
-                                                                        pack_bf16(p[8 * u + 4], p[8 * u + 5]), pack_bf16(p[8 * u + 6], p[8 * u + 7])));
+                const bf16x8 pb = __builtin_bit_cast(bf16x8, make_uint4(packed[4 * u], packed[4 * u + 1], packed[4 * u + 2], packed[4 * u + 3]));
 #pragma unroll
                 for (int b = 0; b < DB; ++b) {
                     acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tr_v_operand<KT, D>(v[u][b]), pb, acc[b], 0, 0, 0);
@@ -490,10 +507,11 @@ __global__ __launch_bounds__(64 * kTrWaves) void tree_kernel(TreeArgs a, TreeSeq
         // Three steps at once: while the matrix unit works on V^T P^T of step i - 1 and K Q^T of step i + 1 in turn, the scores of step i
         // become weights, a share of them behind each instruction, and the operands of the next turn are read from LDS as theirs
         // are used up.  (Between two matrix instructions there is room for six or so vector ones; left to itself the compiler puts
-        // the phases one after the other.)  32 trees of 64 nodes over 8 Ki tokens, 64/8 heads of 128: 558 -> 528 us, 1045 TFLOP/s -- the
-        // chip holds 1.9 GHz under it, and without the copies, on what LDS holds, it takes 462; heads of 64: 406 -> 399.  e4m3 keeps the
-        // steps apart: four conversions more per matrix instruction do not fit between two (530 us; 545 this way).  A ring of five slots, for step i + 2 is
-        // waited for when step i begins.
+        // the phases one after the other.)  32 trees of 64 nodes over 8 Ki tokens, 64/8 heads of 128, when this was put in: 558 -> 528 us,
+        // 1045 TFLOP/s at 1.67 GHz, 462 without the copies, on what LDS holds; heads of 64 406 -> 399.  With the weights added up as they are
+        // rounded 564: what stands between a product of P and one of K delays the latter's chain, so the pair is packed and added behind those of K
+        // (behind those of P 15 us more in a batch of 276).  e4m3 keeps the steps apart: four conversions more per matrix instruction do not
+        // fit between two (530 us; 545 this way).  A ring of five slots, for step i + 2 is waited for when step i begins.
         if (n_plain > 0) {
             constexpr int NQ = D / 16, NP = 2 * DB, SLOTS = NQ + NP, PER = 16 / SLOTS;
             f32x16 x = {};
@@ -530,8 +548,10 @@ __global__ __launch_bounds__(64 * kTrWaves) void tree_kernel(TreeArgs a, TreeSeq
 #pragma unroll
                     for (int e = PER * j; e < PER * (j + 1); ++e) {
                         p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], c, -m));
-                        t[e & 3] += p[e];
-                        if (e % 2 == 1) packed[e / 2] = pack_bf16(p[e - 1], p[e]);
+                        if (e % 2 == 1) {
+                            packed[e / 2] = pack_bf16(p[e - 1], p[e]);
+                            t[e / 2 & 3] = add_pair(packed[e / 2], t[e / 2 & 3]);
+                        }
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
@@ -543,8 +563,10 @@ __global__ __launch_bounds__(64 * kTrWaves) void tree_kernel(TreeArgs a, TreeSeq
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], c, -m));
-                        sum += p[e];
-                        if (e % 2 == 1) packed[e / 2] = pack_bf16(p[e - 1], p[e]);
+                        if (e % 2 == 1) {
+                            packed[e / 2] = pack_bf16(p[e - 1], p[e]);
+                            sum = add_pair(packed[e / 2], sum);
+                        }
                     }
                 }
                 l += sum;

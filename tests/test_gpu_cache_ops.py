@@ -899,3 +899,33 @@ def test_refusal_of_key_numbers_beyond_int32():
     ctx.close()
     torch.cuda.synchronize()
     assert not t.any()
+
+
+@pytest.mark.parametrize("dtype,kind", KINDS)
+@pytest.mark.parametrize("heads", [(8, 2, 64), (64, 8, 128)])
+@pytest.mark.parametrize("shape", [([5], [3005]), ([64] * 4, [700] * 4), ([16, 3, 30], [1800, 900, 40])])
+def test_tree_attention_weights_add_up(dtype, kind, heads, shape):
+    """V is the same for every key, so that the output is V whatever the weights: numerator and denominator take the same ones.  One key a
+    page has a larger score, all others have one score, so that a row's weights are all rounded alike (a share of up to 2^-8 of 16-bit ones).
+    Bound: the sums over n keys are off by n 2^-24 twice, with a dozen roundings besides 4.4e-4 at the most; V is a number of q's type, and
+    the next one is 2^-8 of it away at the least, so that 16-bit outputs are V itself."""
+    b = Batch(heads, dtype, kind, *shape, seed=97)
+    if kind == "fp8":                                      # (powers of two: V times its scale is a bf16 number)
+        b.k_scale, b.v_scale = torch.full((b.Hkv,), 2.0 ** -6), torch.full((b.Hkv,), 2.0 ** -5)
+    unit = 64 if kind == "fp8" else 1
+    sign = torch.randint(0, 2, (b.D,), generator=b.gen).double().numpy() * 2 - 1
+    row = b.cache_of(torch.randn((b.Hkv, b.D), generator=b.gen)).double().numpy()
+    caches = [b.numbers(0).copy(), b.numbers(1).copy()]
+    for s, n in enumerate(b.ctx_lens):
+        pos = np.arange(n)
+        caches[0][places("k", b.table, np.full(n, s), pos, b.Hkv, b.D, kind)] = \
+            np.where(pos % PAGE == 0, 1.0, 0.25)[:, None, None] * unit * sign
+        caches[1][places("v", b.table, np.full(n, s), pos, b.Hkv, b.D, kind)] = row
+    caches = [torch.from_numpy(c).to(torch.float32).to(b.caches[0].dtype) for c in caches]
+    size = 0.02 + 0.4 * torch.rand((b.T, b.Hq, 1), generator=b.gen)
+    q = (size.to(TORCH[dtype]).double() * torch.from_numpy(sign)).to(TORCH[dtype])
+    rng = np.random.default_rng(15)
+    see = [tree_see(random_tree(rng, n)) for n in b.q_lens]
+    want = np.repeat(row * (2.0 ** -5 if kind == "fp8" else 1.0), b.Hq // b.Hkv, 0)[None].repeat(b.T, 0)
+    bound = np.abs(want) * 2 * (int(b.ctx_lens.max()) + 12) * 2.0 ** -24 if dtype == "f32" else np.zeros_like(want)
+    check(tree_run(b, q, see, caches=caches), want, bound)
