@@ -1345,11 +1345,11 @@ extern "C" int ts_rope_kv_append(ts_ctx* c, void* stream, const void* q, int64_t
         const int64_t qw = (int64_t)c->desc.num_q_heads * c->desc.head_dim, kw = (int64_t)c->desc.num_kv_heads * c->desc.head_dim;
         if ((q_stride != 0 && q_stride < qw) || (k_stride != 0 && k_stride < kw) || (v_stride != 0 && v_stride < kw))
             return fail(c, TS_ERR_INVALID_ARG, "a stride is smaller than a token's row");
-        if ((q == nullptr) != (q_out == nullptr)) return fail(c, TS_ERR_INVALID_ARG, "q and q_out must both be given or both be NULL");
-        if (q && q == q_out && q_stride != 0 && q_stride != qw) return fail(c, TS_ERR_INVALID_ARG, "q_out may be q only if its rows are packed");
         int64_t total = 0;
         for (int s = 0; s < num_seqs; ++s) total += q_lens[s];
-        if (total == 0) return TS_OK;
+        if (total == 0) return TS_OK;                      // (no row of q to be given, whatever q_out is)
+        if ((q == nullptr) != (q_out == nullptr)) return fail(c, TS_ERR_INVALID_ARG, "q and q_out must both be given or both be NULL");
+        if (q && q == q_out && q_stride != 0 && q_stride != qw) return fail(c, TS_ERR_INVALID_ARG, "q_out may be q only if its rows are packed");
         if (!k_new || !v_new) return fail(c, TS_ERR_INVALID_ARG, "k_new / v_new is NULL");
         DeviceGuard guard(c->device);
         Op op{c, (hipStream_t)stream};

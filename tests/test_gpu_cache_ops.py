@@ -929,3 +929,32 @@ def test_tree_attention_weights_add_up(dtype, kind, heads, shape):
     want = np.repeat(row * (2.0 ** -5 if kind == "fp8" else 1.0), b.Hq // b.Hkv, 0)[None].repeat(b.T, 0)
     bound = np.abs(want) * 2 * (int(b.ctx_lens.max()) + 12) * 2.0 ** -24 if dtype == "f32" else np.zeros_like(want)
     check(tree_run(b, q, see, caches=caches), want, bound)
+
+
+@pytest.mark.parametrize("dtype,kind", KINDS)
+def test_steps_without_tokens(dtype, kind):
+    """No sequence brings a token, the buffers are there all the same (a serving loop's, of its largest batch): nothing is done, nothing is
+    refused, through the binding and through the C entry points."""
+    b = Batch((8, 2, 64), dtype, kind, [3, 2], [20, 40], seed=98)
+    ctx, lib = ts.Context(b.desc()), ts.load_library()
+    ctx.set_rope(64)
+    kc, vc, ks, vs, table = b.on_gpu()
+    q, k, v = (b.randn(b.T, h, 64).cuda() for h in (8, 2, 2))
+    out, ko, vo = (torch.full((b.T, h, 64), 7.0, dtype=TORCH[dtype], device="cuda") for h in (8, 2, 2))
+    before = [t.clone() for t in (kc, vc, q)]
+    i5, mask = torch.zeros(5, dtype=torch.int32, device="cuda"), torch.zeros((b.T, 1), dtype=torch.int64, device="cuda")
+    for lens in ([0, 0], []):
+        cl, tab = b.ctx_lens[:len(lens)], table[:len(lens)]
+        ctx.rope_kv_append(q, k, v, out, kc, vc, ks, vs, tab, lens, cl)
+        ctx.rope_kv_append(q, k, v, q, kc, vc, ks, vs, tab, lens, cl, positions=i5)
+        ctx.rope_kv_append(None, k, v, None, kc, vc, ks, vs, tab, lens, cl)
+        ctx.tree_attention(q, kc, vc, ks, vs, tab, mask, lens, cl, 0.0, out)
+        ctx.kv_move(kc, vc, tab, i5, i5, lens, cl)
+        ctx.kv_read(kc, vc, ks, vs, tab, None, lens, ko, vo)
+    zero, cl = np.zeros(2, np.int32).tobytes(), b.ctx_lens.tobytes()
+    p = [t.data_ptr() if t is not None else 0 for t in (kc, vc, ks, vs, table)]
+    assert lib.ts_rope_kv_append(ctx._h, 0, None, 0, None, 0, None, 0, out.data_ptr(), *p, 0, zero, cl, 2) == binding.TS_OK
+    assert lib.ts_rope_kv_append(ctx._h, 0, q.data_ptr(), 0, k.data_ptr(), 0, v.data_ptr(), 0, out.data_ptr(), *p, 0, zero, cl, 2) == binding.TS_OK
+    torch.cuda.synchronize()
+    assert all((t == 7.0).all() for t in (out, ko, vo)) and all(torch.equal(x, y) for x, y in zip((kc, vc, q), before))
+    ctx.close()
