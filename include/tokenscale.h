@@ -273,7 +273,7 @@ int ts_kv_move(ts_ctx *ctx, void *stream, void *k_cache, void *v_cache, const in
 /* Reads cached tokens back as rows: positions starts[s] .. starts[s] + lens[s] - 1 of every sequence, packed by sequence.
  *   k_out, v_out : DEV [sum of lens, Hkv, D] q_dtype; one of them may be NULL.  e4m3 elements are multiplied by their head's
  *                  scale in single precision and rounded once
- *   starts, lens : HOST int32 [S], starts may be NULL (0)
+ *   starts, lens : HOST int32 [S], starts may be NULL (0).  Only the pages that hold these positions are looked up in block_table
  * Errors: TS_ERR_INVALID_ARG for null pointers, negative numbers, positions beyond the table. */
 int ts_kv_read(ts_ctx *ctx, void *stream, const void *k_cache, const void *v_cache,
                const float *k_scale, const float *v_scale, const int32_t *block_table,

@@ -1240,7 +1240,8 @@ struct OpGuard {
     ~OpGuard() { if (!done) (void)op.finish(false); }
 };
 
-// Option "validate_block_table" for these calls: pages(i) = pages that sequence i uses.
+// Option "validate_block_table" for these calls: pages(i) = pages that sequence i uses, the first and the one behind the last.
+struct PageRange { int32_t from, to; };
 template <typename F>
 int check_op_pages(Op& op, const int32_t* block_table, int num_seqs, F&& pages)
 {
@@ -1253,7 +1254,11 @@ int check_op_pages(Op& op, const int32_t* block_table, int num_seqs, F&& pages)
         PageCheck p{};
         p.n = std::min(kPageCheckSeqs, num_seqs - s0);
         p.first = s0;
-        for (int i = 0; i < p.n; ++i) p.pages[i] = pages(s0 + i);
+        for (int i = 0; i < p.n; ++i) {
+            const PageRange r = pages(s0 + i);
+            p.from[i] = r.from;
+            p.to[i] = r.to;
+        }
         TS_HIP(c, (hipError_t)launch_check_pages(p, block_table, c->desc.max_pages_per_seq, c->desc.num_pages, res, op.st));
     }
     int32_t host[4] = {0, 0, 0, 0};
@@ -1355,7 +1360,7 @@ extern "C" int ts_rope_kv_append(ts_ctx* c, void* stream, const void* q, int64_t
         Op op{c, (hipStream_t)stream};
         rc = op.begin();
         if (rc != TS_OK) return rc;
-        rc = check_op_pages(op, block_table, num_seqs, [&](int s) { return pages_up_to(ctx_lens[s]); });
+        rc = check_op_pages(op, block_table, num_seqs, [&](int s) { return PageRange{0, pages_up_to(ctx_lens[s])}; });
         if (rc != TS_OK) return rc;
         RopeArgs a{};
         a.geo = geometry_of(c->desc);
@@ -1455,7 +1460,7 @@ extern "C" int ts_tree_attention(ts_ctx* c, void* stream, const void* q, const v
             rc = ts_reserve_tree(c);
             if (rc != TS_OK) return rc;
         }
-        rc = check_op_pages(op, block_table, num_seqs, [&](int s) { return q_lens[s] > 0 ? pages_up_to(ctx_lens[s]) : 0; });
+        rc = check_op_pages(op, block_table, num_seqs, [&](int s) { return PageRange{0, q_lens[s] > 0 ? pages_up_to(ctx_lens[s]) : 0}; });
         if (rc != TS_OK) return rc;
         TreeArgs a{};
         a.geo = geometry_of(c->desc);
@@ -1527,7 +1532,7 @@ extern "C" int ts_kv_move(ts_ctx* c, void* stream, void* k_cache, void* v_cache,
         Op op{c, (hipStream_t)stream};
         rc = op.begin();
         if (rc != TS_OK) return rc;
-        rc = check_op_pages(op, block_table, num_seqs, [&](int s) { return move_lens[s] > 0 ? pages_up_to(ctx_lens[s]) : 0; });
+        rc = check_op_pages(op, block_table, num_seqs, [&](int s) { return PageRange{0, move_lens[s] > 0 ? pages_up_to(ctx_lens[s]) : 0}; });
         if (rc != TS_OK) return rc;
         MoveArgs a{};
         a.geo = geometry_of(c->desc);
@@ -1584,7 +1589,10 @@ extern "C" int ts_kv_read(ts_ctx* c, void* stream, const void* k_cache, const vo
         Op op{c, (hipStream_t)stream};
         rc = op.begin();
         if (rc != TS_OK) return rc;
-        rc = check_op_pages(op, block_table, num_seqs, [&](int s) { return lens[s] > 0 ? pages_up_to((starts ? (int64_t)starts[s] : 0) + lens[s]) : 0; });
+        rc = check_op_pages(op, block_table, num_seqs, [&](int s) {
+            const int32_t start = starts ? starts[s] : 0;
+            return lens[s] > 0 ? PageRange{start / kPage, pages_up_to((int64_t)start + lens[s])} : PageRange{0, 0};
+        });
         if (rc != TS_OK) return rc;
         ReadArgs a{};
         a.geo = geometry_of(c->desc);

@@ -353,8 +353,9 @@ struct ReadArgs {
     int32_t first_unit;
 };
 
-struct PageCheck { int32_t n, first; int32_t pages[512]; };     // pages that sequence first + i uses
-constexpr int kPageCheckSeqs = 512;
+constexpr int kPageCheckSeqs = 448;
+struct PageCheck { int32_t n, first; int32_t from[kPageCheckSeqs], to[kPageCheckSeqs]; };     // sequence first + i uses pages from[i] .. to[i] - 1
+static_assert(sizeof(PageCheck) + 64 <= 4096, "kernel arguments");
 
 // ---- attention of drafted trees ----------------------------------------------------------------
 

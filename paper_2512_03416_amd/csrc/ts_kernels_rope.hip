@@ -587,7 +587,7 @@ __global__ __launch_bounds__(256) void check_pages_few_kernel(PageCheck c, const
                                                               int32_t* result)
 {
     const int s = blockIdx.x;
-    for (int p = threadIdx.x; p < c.pages[s]; p += blockDim.x) {
+    for (int p = c.from[s] + threadIdx.x; p < c.to[s]; p += blockDim.x) {
         const int32_t id = bt[(int64_t)(c.first + s) * max_pages + p];
         if (id < 0 || id >= num_pages) {
             if (atomicAdd(&result[0], 1) == 0) { result[1] = c.first + s; result[2] = p; }

@@ -958,3 +958,31 @@ def test_steps_without_tokens(dtype, kind):
     torch.cuda.synchronize()
     assert all((t == 7.0).all() for t in (out, ko, vo)) and all(torch.equal(x, y) for x, y in zip((kc, vc, q), before))
     ctx.close()
+
+
+def test_read_checks_the_pages_that_it_reads():
+    """Option validate_block_table: pages in front of the tokens that are read may be gone (-1), as may those behind them."""
+    b = Batch((8, 2, 64), "bf16", "bf16", [0, 0], [200, 90], seed=99)
+    ctx = ts.Context(b.desc())
+    kc, vc, ks, vs, table = b.on_gpu()
+    starts, lens = [70, 33], [50, 31]                      # pages 4 .. 7 and 2 .. 3
+    rows = lambda: [torch.full((81, 2, 64), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]  # noqa: E731
+    want, got, refused = rows(), rows(), rows()
+    ctx.kv_read(kc, vc, ks, vs, table, starts, lens, *want)
+    ctx.set_option("validate_block_table", 1)
+    holes = torch.full_like(table, -1)
+    for s, (first, behind) in enumerate(((4, 8), (2, 4))):
+        holes[s, first:behind] = table[s, first:behind]
+    ctx.kv_read(kc, vc, ks, vs, holes, starts, lens, *got)
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        assert torch.equal(g, w)
+    for s, page, bad in ((0, 4, -1), (0, 7, b.pool), (1, 2, b.pool), (1, 3, -1)):
+        wrong = holes.clone()
+        wrong[s, page] = bad
+        with pytest.raises(ts.TokenScaleError) as e:
+            ctx.kv_read(kc, vc, ks, vs, wrong, starts, lens, *refused)
+        assert e.value.code == binding.TS_ERR_INVALID_ARG and f"sequence {s}, page {page}" in str(e.value)
+    torch.cuda.synchronize()
+    assert all((t == 7.0).all() for t in refused)
+    ctx.close()
