@@ -3,6 +3,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import sys
 from typing import Optional, Sequence
 
 import numpy as np
@@ -311,15 +312,23 @@ class Context:
         self.device = device
         self._cache_bytes = cache_bytes(desc)
         self._hq, self._hkv, self._dim, self._width = desc.num_q_heads, desc.num_kv_heads, desc.head_dim, desc.max_pages_per_seq
-        import torch
-        self._f32, self._i32, self._i64 = torch.float32, torch.int32, torch.int64
-        self._q_type = torch.float32 if desc.q_dtype == DTYPES["f32"] else torch.bfloat16
         self._h = ctypes.c_void_p(0)
         rc = self._lib.ts_create(ctypes.byref(desc), device, ctypes.byref(self._h))
         if rc != TS_OK:
             msg = self._lib.ts_last_error(ctypes.c_void_p(0)).decode()
             self._h = ctypes.c_void_p(0)
             raise TokenScaleError(rc, msg)
+
+    def __getattr__(self, name):
+        # torch's types, which become attributes once torch is there.  Before, no argument can be a tensor, and none is compared.
+        if name not in ("_f32", "_i32", "_i64", "_q_type"):
+            raise AttributeError(name)
+        torch = sys.modules.get("torch")
+        if torch is None:
+            return None
+        self._f32, self._i32, self._i64 = torch.float32, torch.int32, torch.int64
+        self._q_type = torch.float32 if self.desc.q_dtype == DTYPES["f32"] else torch.bfloat16
+        return self.__dict__[name]
 
     def close(self):
         if self._h:

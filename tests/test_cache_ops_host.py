@@ -4,6 +4,7 @@ import math
 import os
 import re
 import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -127,3 +128,72 @@ def test_kernels_keep_their_values_in_registers():
                 if m and name:
                     assert int(m.group(1)) <= most, (name, line)
     assert len(names - {""}) == 7
+
+
+def test_a_context_of_raw_pointers_needs_no_torch():
+    """Device pointers and a stream handle as integers: nothing imports torch, which here cannot be imported (the library's calls are
+    stood in for, there being no GPU)."""
+    code = """
+import ctypes, sys
+sys.modules["torch"] = None
+from paper_2512_03416_amd import binding
+binding.load_library()
+class Calls:
+    made = []
+    def __getattr__(self, name):
+        if name == "ts_cache_bytes":
+            return lambda d: 1 << 20
+        return lambda *a: self.made.append((name, a)) or 0
+binding._lib = Calls()
+c = binding.Context(binding.Desc.make(8, 2, 64, "bf16", "bf16", 8, 4))
+page = 1 << 20
+c.set_rope(64)
+c.kv_append(page, page, page, page, None, None, page, [3], [20], stream=0)
+c.mixed_paged_attention(page, None, None, page, page, None, None, page, [3], [20], 0.0, page, stream=0)
+c.tree_attention(page, page, page, None, None, page, None, [3], [20], 0.0, page, stream=0)
+c.kv_move(page, page, page, page, page, [3], [20], stream=0)
+c.kv_read(page, page, page, page, page, None, [3], page, page, stream=0)
+print(" ".join(name for name, a in Calls.made))
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert r.returncode == 0, r.stderr[-2000:]
+    assert r.stdout.split() == ["ts_create", "ts_set_rope", "ts_kv_append", "ts_mixed_paged_attention", "ts_tree_attention", "ts_kv_move", "ts_kv_read"]
+
+
+def test_tensors_are_checked_whenever_torch_was_loaded():
+    """A context made before torch is loaded checks tensors as any other."""
+    code = """
+import sys
+from paper_2512_03416_amd import binding
+binding.load_library()
+class Calls:
+    def __getattr__(self, name):
+        return lambda *a: 1 << 20 if name == "ts_cache_bytes" else 0
+binding._lib = Calls()
+assert "torch" not in sys.modules
+c = binding.Context(binding.Desc.make(8, 2, 64, "bf16", "bf16", 8, 4), device=-1)      # (-1: where CPU tensors are)
+c.kv_move(1, 1, 1, 1, 1, [3], [20], stream=0)
+assert "torch" not in sys.modules
+import torch
+i5, i8, f5 = torch.zeros(5, dtype=torch.int32), torch.zeros(8, dtype=torch.int64), torch.zeros(5)
+c.kv_move(1, 1, 1, i5, i5, [3], [20], stream=0)
+for bad in (i8, f5):
+    try:
+        c.kv_move(1, 1, 1, i5, bad, [3], [20], stream=0)
+    except ValueError as e:
+        assert "expected torch.int32" in str(e), e
+    else:
+        raise AssertionError(bad.dtype)
+q = torch.zeros((3, 8, 64), dtype=torch.bfloat16)
+c.tree_attention(q, 1, 1, None, None, 1, torch.zeros((3, 1), dtype=torch.int64), [3], [20], 0.0, q, stream=0)
+for bad in ((q.float(), None), (q, i5.view(5, 1))):
+    try:
+        c.tree_attention(bad[0], 1, 1, None, None, 1, bad[1], [3], [20], 0.0, q, stream=0)
+    except ValueError as e:
+        assert "expected torch." in str(e), e
+    else:
+        raise AssertionError(bad)
+print("ok")
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert r.returncode == 0 and r.stdout.strip() == "ok", r.stderr[-2000:]
