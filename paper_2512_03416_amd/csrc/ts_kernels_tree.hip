@@ -543,7 +543,7 @@ __global__ __launch_bounds__(64 * kTrWaves) void tree_kernel(TreeArgs a, TreeSeq
                         v[u][b] = tr_load_v<KT, D>(lv, u, b, lane);
                     } else {
                         x_next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tr_k_operand<KT, D>(k, o), q.q[o], x_next, 0, 0, 0);
-                        if (sizeof(KT) == 2 || o % 2 == 1) k.piece[sizeof(KT) == 2 ? o : o / 2] = *(const uint4*)(lk + (sizeof(KT) == 2 ? o : o / 2) * 512);
+                        k.piece[o] = *(const uint4*)(lk + o * 512);
                     }
 #pragma unroll
                     for (int e = PER * j; e < PER * (j + 1); ++e) {
@@ -668,9 +668,9 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, TreeSeqs s,
         const int k = min(b + lane, kTreeSeqs - 1);
         i += __builtin_popcountll(__ballot((b + lane < s.n) & (s.seq[k].first_merge <= w)));
     }
-    // (sequences that were not cut share the number of the next one that was: the last match counts, unless it is one behind the last cut one)
-    TreeSeq q = s.seq[i];
-    while (q.parts < 2) q = s.seq[--i];
+    // (a sequence that was not cut has the number of the next one that was, or, behind the last of them, that of all rows, which w is below:
+    // the last match is one that was cut)
+    const TreeSeq q = s.seq[i];
     const int rows = q.n_nodes * a.geo.G, k = w - q.first_merge, g = k / rows, row = k % rows;
     const int64_t at = q.part_row0 + (int64_t)g * q.parts * rows + row;
     float top = kNoKeyTr, sum = 0.0f;
