@@ -986,3 +986,60 @@ def test_read_checks_the_pages_that_it_reads():
     torch.cuda.synchronize()
     assert all((t == 7.0).all() for t in refused)
     ctx.close()
+
+
+@pytest.mark.parametrize("dtype,kind", KINDS)
+def test_validated_calls_give_the_same(dtype, kind):
+    """Option validate_block_table on good tables: outputs and caches as without it, over more sequences than one check takes."""
+    n = 600
+    rng = np.random.default_rng(16)
+    ql = rng.integers(0, 4, n)
+    b = Batch((8, 2, 64), dtype, kind, ql, ql + rng.integers(0, 60, n), seed=100)
+    see = [tree_see(random_tree(rng, m)) if m else np.zeros((0, 0), bool) for m in ql]
+    q, k, v = (b.randn(b.T, h, 64).cuda() for h in (8, 2, 2))
+    mask = mask_on_gpu(see)
+    moves = np.minimum(ql, 2)
+    src, dst = (torch.from_numpy(rng.integers(0, np.repeat(b.ctx_lens, moves)).astype(np.int32)).cuda() for _ in range(2))
+    starts = rng.integers(0, b.ctx_lens + 1)
+    lens = b.ctx_lens - starts
+    runs = []
+    for validate in (0, 1):
+        ctx = ts.Context(b.desc())
+        ctx.set_rope(64)
+        ctx.set_option("validate_block_table", validate)
+        kc, vc, ks, vs, table = b.on_gpu()
+        turned, out = (torch.full((b.T, 8, 64), 7.0, dtype=TORCH[dtype], device="cuda") for _ in range(2))
+        rows = [torch.full((int(lens.sum()), 2, 64), 7.0, dtype=TORCH[dtype], device="cuda") for _ in range(2)]
+        ctx.rope_kv_append(q, k, v, turned, kc, vc, ks, vs, table, b.q_lens, b.ctx_lens)
+        ctx.tree_attention(turned, kc, vc, ks, vs, table, mask, b.q_lens, b.ctx_lens, 0.0, out)
+        ctx.kv_move(kc, vc, table, src, dst, moves, b.ctx_lens)
+        ctx.kv_read(kc, vc, ks, vs, table, starts, lens, *rows)
+        torch.cuda.synchronize()
+        runs.append([bits(t) for t in (turned, out, kc, vc, *rows)])
+        ctx.close()
+    for x, y in zip(*runs):
+        assert np.array_equal(x, y)
+    assert not np.array_equal(runs[1][2], bits(b.caches[0]))
+
+
+@pytest.mark.parametrize("dtype,kind", KINDS)
+@pytest.mark.parametrize("empty", [(64, 192), (0, 64), (384, 768), (0, 384), (320, 900)])
+def test_blocks_of_sequences_without_tokens(dtype, kind, empty):
+    """Append and read where whole aligned blocks of 64 sequences, or the 384 of a launch, bring no token."""
+    n = 900
+    rng = np.random.default_rng(17)
+    ql = rng.integers(1, 4, n)
+    ql[empty[0]:empty[1]] = 0
+    b = Batch((4, 1, 64), dtype, kind, ql, ql + rng.integers(0, 40, n), seed=101)
+    rope_case(b, ROPES[1], b.randn(b.T, 4, 64), b.randn(b.T, 1, 64), b.randn(b.T, 1, 64), strided=True, positions=None)
+    ctx = ts.Context(b.desc())
+    kc, vc, ks, vs, table = b.on_gpu()
+    rows = [torch.empty((b.T, 1, 64), dtype=TORCH[dtype], device="cuda") for _ in range(2)]
+    ctx.kv_read(kc, vc, ks, vs, table, b.ctx_lens - b.q_lens, b.q_lens, *rows)
+    torch.cuda.synchronize()
+    for i, got in enumerate(rows):
+        want = b.caches[i].float()[torch.from_numpy(places("kv"[i], b.table, b.seq, b.pos, 1, 64, kind))]
+        if kind == "fp8":
+            want = (want * (b.k_scale, b.v_scale)[i][None, :, None]).to(TORCH[dtype])
+        assert torch.equal(got.cpu().float(), want.float())
+    ctx.close()
