@@ -1043,3 +1043,23 @@ def test_blocks_of_sequences_without_tokens(dtype, kind, empty):
             want = (want * (b.k_scale, b.v_scale)[i][None, :, None]).to(TORCH[dtype])
         assert torch.equal(got.cpu().float(), want.float())
     ctx.close()
+
+
+@pytest.mark.parametrize("heads", [(4, 1, 64), (64, 8, 128)])
+@pytest.mark.parametrize("nodes,prefix", [(4, 0), (4, 600), (60, 700)])
+def test_tree_attention_infinite_scores_in_16_bits(heads, nodes, prefix):
+    """Every key of the prefix and the first node have a score of -inf, the second node a finite one, the third one +inf: a row that sees the
+    first node only is NaN, one that sees the second too has its V, one that sees the third is NaN."""
+    b = Batch(heads, "bf16", "bf16", [nodes], [prefix + nodes], seed=102)
+    k = b.caches[0].clone()
+    at = places("k", b.table, np.zeros(prefix + 1, int), np.arange(prefix + 1), b.Hkv, b.D, b.kind)
+    k[torch.from_numpy(at[:, :, 5].reshape(-1))] = -float("inf")
+    k[torch.from_numpy(places("k", b.table, np.array([0]), np.array([prefix + 2]), b.Hkv, b.D, b.kind)[:, :, 5].reshape(-1))] = float("inf")
+    see = np.zeros((nodes, nodes), bool)
+    see[:, 0] = True
+    see[1::3, 1] = True
+    see[2::3, 1:3] = True
+    got = tree_run(b, torch.ones((nodes, b.Hq, b.D)).to(torch.bfloat16), [see], caches=[k, b.caches[1]]).cpu()
+    assert torch.isnan(got[0::3]).all() and torch.isnan(got[2::3]).all()
+    v = torch.from_numpy(b.tokens(1, 0, prefix + 2)[-1]).repeat_interleave(b.Hq // b.Hkv, 0)
+    assert (got[1::3].double() == v).all()                 # (a weight of one, whatever the reference: nothing is rounded)
