@@ -168,7 +168,8 @@ int ts_mixed_paged_attention_noalloc(ts_ctx *ctx, void *stream,
  * Conventions as above, and: these calls allocate nothing on the device but ts_tree_attention's scratch (see
  * ts_reserve_tree), use no pinned memory and keep no lists on the device, so all of them may be captured into a graph; a
  * captured call fixes the HOST arrays' values.  A context orders its eager calls among streams; the replays of its graphs,
- * which share its scratch, are ordered by the caller.  k_cache and v_cache must be 16-byte aligned.  "kernel_timing" counts the append, move and read under TS_K_APPEND, the tree attention under
+ * which share its scratch, are ordered by the caller.  k_cache and v_cache must be 16-byte aligned.  A batch without tokens
+ * (or pairs) is no error.  "kernel_timing" counts the append, move and read under TS_K_APPEND, the tree attention under
  * TS_K_DECODE and its merge under TS_K_COMBINE (eager calls only); "validate_block_table" is honoured, but refused under
  * capture (TS_ERR_UNSUPPORTED).  None of them touches the velocity counters. */
 
@@ -248,7 +249,8 @@ int ts_tree_attention(ts_ctx *ctx, void *stream,
                       const int32_t *q_lens, const int32_t *ctx_lens, int num_seqs,
                       float sm_scale, void *out);
 
-/* Allocates ts_tree_attention's scratch (its size goes by the geometry, not by the batch: at most 160 MiB) if it is not there yet.
+/* Allocates ts_tree_attention's scratch (its size goes by the geometry, not by the batch: 130 MiB with
+ * 128 dims, 66 with 64) if it is not there yet.
  * Without it the first call that needs it allocates it, which fails with TS_ERR_UNSUPPORTED under capture. */
 int ts_reserve_tree(ts_ctx *ctx);
 

@@ -509,8 +509,8 @@ __global__ __launch_bounds__(64 * kTrWaves) void tree_kernel(TreeArgs a, TreeSeq
         // are used up.  (Between two matrix instructions there is room for six or so vector ones; left to itself the compiler puts
         // the phases one after the other.)  32 trees of 64 nodes over 8 Ki tokens, 64/8 heads of 128, when this was put in: 558 -> 528 us,
         // 1045 TFLOP/s at 1.67 GHz, 462 without the copies, on what LDS holds; heads of 64 406 -> 399.  With the weights added up as they are
-        // rounded 564: what stands between a product of P and one of K delays the latter's chain, so the pair is packed and added behind those of K
-        // (behind those of P 15 us more in a batch of 276).  e4m3 keeps the steps apart: four conversions more per matrix instruction do not
+        // rounded 564, with the pair packed and added behind the products of K (behind those of P a batch of 288 us takes 301 to 314, all pairs at the
+        // step's end 300).  e4m3 keeps the steps apart: four conversions more per matrix instruction do not
         // fit between two (530 us; 545 this way).  A ring of five slots, for step i + 2 is waited for when step i begins.
         if (n_plain > 0) {
             constexpr int NQ = D / 16, NP = 2 * DB, SLOTS = NQ + NP, PER = 16 / SLOTS;

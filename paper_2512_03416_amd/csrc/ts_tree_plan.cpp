@@ -110,8 +110,8 @@ static TreeTimes tree_times(const ts_attn_desc& d, int rows, int n_cu)
     const int per_cu = std::max(1, std::min(2, 160 * 1024 / (slot * tree_ring_slots(slot, elem == 2))));
     t.places = (int64_t)n_cu * per_cu;
     t.page_alone = 0.36 * rows / 128 * (0.3 + 0.7 * dims) * math;
-    // 32 trees of 64 nodes over 8 Ki tokens (64/8 heads of 128): bf16 528 us with 128 rows, 630 with 64, 1015 with 32 (one workgroup per CU, and
-    // L2 reads of 17 TB/s), e4m3 530, 564, 628; 8 trees of 100-128 nodes over 2-9 Ki, e4m3: 208, 187, 199
+    // 32 trees of 64 nodes over 8 Ki tokens (64/8 heads of 128): bf16 556 us with 128 rows, 652 with 64, 1007 with 32 (one workgroup per CU, and
+    // L2 reads of 17 TB/s), e4m3 546, 572, 642; 8 trees of 100-128 nodes over 2-9 Ki, e4m3: 209, 186, 198
     const bool e4m3 = elem == 1;
     t.page_full = (rows == 32 ? (per_cu == 1 ? 0.118 : (e4m3 ? 0.155 : 0.16)) : (rows == 64 ? (per_cu == 1 ? 0.2 : (e4m3 ? 0.288 : 0.335)) : (per_cu == 1 ? 0.36 : (e4m3 ? 0.525 : 0.49)))) * dims * math;
     t.page_read = 2.0 * kPage * d.head_dim * elem / 6.2e6;     // 6.2 TB/s
@@ -130,7 +130,8 @@ static TreeTimes tree_times(const ts_attn_desc& d, int rows, int n_cu)
 // comes out even by itself: 32 trees of 32-64 nodes over 1-8 Ki tokens (64/8 heads) took 287 us uncut, 312 in ranges of at most 384
 // pages, 325 in ranges of 192.  Smaller batches are cut until the workgroups fill the places: 8 trees of 30 nodes over 4000 tokens
 // (32/8 heads, 128 rows) 92 us uncut, 39 to 41 in ranges of 32 to 64 pages, 53 in ranges of 16 (most of it partial results).  Ranges of a sequence
-// are of one length.  Both are taken from the times above, which come within 8 % of the best number of rows on these batches and 22 more.
+// are of one length.  Both are taken from the times above.  On 29 of 30 batches of 16-bit queries the number of rows that they choose is within 8 % of the
+// best one's time, on one 10 %; on 15 of fp32, whose page times are the 16-bit ones eight times over, within 16 %.
 void plan_tree(const ts_attn_desc& d, const int32_t* q_lens, const int32_t* ctx_lens, int num_seqs, int n_cu, TreePlan* plan)
 {
     const int32_t G = d.num_q_heads / d.num_kv_heads, Hkv = d.num_kv_heads;
